@@ -221,8 +221,9 @@ def prepare(case, seed):
                   parent=None if parent is None else _dev(parent))
         for name, shape, t in (("row_start", (B + 1,), torch.int32), ("slot", (rows,), torch.int32),
                                ("coords", (rows, 3), torch.int32), ("n_blocks_out", (B,), torch.int32),
-                               ("free_head_out", (1,), torch.int32), ("status", (1,), torch.int32)):
+                               ("free_head_out", (1,), torch.int32)):
             st[name] = torch.empty(shape, dtype=t, device="cuda")
+        st["status"] = torch.zeros(1, dtype=torch.int32, device="cuda")  # flags are added to it
         st["mask"] = torch.empty((rows, words), dtype=torch.int64, device="cuda") if c["tree"] else None
     else:
         pos = cached[req] + idx
@@ -336,7 +337,7 @@ def _plain_plan(st):
     at = (first[:, None] + col - held[:, None]).clamp(0, st["free"].numel() - 1)
     st["table"].copy_(torch.where(take, st["free"][at], st["table"]))
     end = st["free_head"].long() + grow.sum()
-    st["status"].copy_((need > st["table"].shape[1]).any().int() * 2 + (end > st["free"].numel()).int() * 4)
+    st["status"].bitwise_or_((need > st["table"].shape[1]).any().int() * 2 + (end > st["free"].numel()).int() * 4)
     st["n_blocks_out"].copy_(held + grow)
     st["free_head_out"].copy_(end)
     r = torch.arange(st["n_rows"], device="cuda")
