@@ -383,6 +383,190 @@ cs_status selective_attend_scatter_rope_paged(const cs_geometry* g, void* const*
                                               void* workspace, size_t workspace_bytes,
                                               void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Answering over composed caches: batches of requests over a pool of pages.
+ *
+ * A page is a chunk buffer of the *_paged calls, [L][H_kv][P][D] with P tokens,
+ * and a pool holds n_pages of them one behind the other, for keys and for
+ * values.  The calls below take the geometry of ONE page (n_tokens = P; its
+ * chunks are not looked at), and a page can be handed to the *_paged calls as
+ * a chunk (k_chunks[c] = k_pages + page x L x H_kv x P x D elements), so a
+ * memory is composed where it lies.
+ *
+ * Token j of request b lies at offset j % P of page block_table[b][j / P].  A
+ * request has cached_len[b] tokens behind it and new_len[b] new ones (rows) in
+ * the step: the next token, a tree of drafted tokens, or a question's tokens.
+ * The rows of all requests follow each other: request b owns rows
+ * [row_start[b], row_start[b + 1]), and its i-th row is its token
+ * cached_len[b] + i.  Which rows a row sees is a bit mask, so a step is
+ *     batch_plan_pages       pages, slots, coordinates and masks (once a step)
+ *     qk_norm_rope_append    per layer: norm, rotation, keys and values to pages
+ *     tree_attend_paged      per layer: attention of the rows
+ *     tree_commit_paged      the rows of an accepted path become cached tokens
+ *
+ * All the arrays of cs_batch are DEVICE memory, dense, and are read when the
+ * stream gets there, so a captured graph can be replayed with new lengths.
+ * Their contents cannot be checked by the host.  Whatever they hold, no call
+ * reads or writes outside the buffers it was given: a table entry or slot
+ * outside the pool is left out (its keys are not seen, its rows not written).
+ * max_rows only chooses between kernels: no results but for rounding depend on
+ * it.  Calls may overlap where one does not write what another uses.  A batch
+ * has at most 4,096 requests (CS_ERR_UNSUPPORTED beyond), and the pool's two
+ * buffers are aligned to 16 bytes.                                         */
+typedef struct {
+  void* k_pages;               /* DEVICE [n_pages][L][H_kv][P][D] */
+  void* v_pages;               /* the same */
+  int64_t n_pages;             /* n_pages x P < 2^31 */
+} cs_page_pool;
+
+typedef struct {
+  int32_t n_requests;          /* B >= 0 */
+  int32_t n_rows;              /* rows the row arrays have room for, >= row_start[B] */
+  int32_t max_blocks;          /* entries of a block table's row */
+  int32_t mask_words;          /* 64-bit words of a mask's row */
+  int32_t max_rows;            /* the most rows one request is expected to have; 0: n_rows */
+  const int32_t* cached_len;   /* [B] */
+  int32_t* row_start;          /* [B + 1] */
+  int32_t* block_table;        /* [B][max_blocks] */
+  int32_t* slot;               /* [n_rows] page x P + offset of every row; -1: none */
+  int32_t* coords;             /* [n_rows][3] (t, h, w) of every row */
+  uint64_t* tree_mask;         /* [n_rows][mask_words]: bit w of row i: row i sees row w of its
+                                  request; NULL: a row sees itself and the rows before it */
+} cs_batch;
+
+/* Rows of heads: element d of head h of row r is data[r x row_stride +
+ * h x head_stride + d] (strides in elements, >= 0), so the slices of a
+ * projection's rows are used where they are.                               */
+typedef struct {
+  void* data;                  /* DEVICE, geometry.dtype */
+  int64_t row_stride, head_stride;
+} cs_rows;
+
+typedef struct {
+  const int32_t* new_len;      /* DEVICE [B] rows of every request, >= 0 */
+  const int32_t* n_blocks;     /* DEVICE [B] pages every request holds */
+  int32_t* n_blocks_out;       /* DEVICE [B] the same after the step; not n_blocks */
+  const int32_t* free_pages;   /* DEVICE [n_free] free pages, taken in order */
+  int32_t n_free;
+  const int32_t* free_head;    /* DEVICE [1] entries of free_pages already taken */
+  int32_t* free_head_out;      /* DEVICE [1] the same after the step; not free_head */
+  const int32_t* parent;       /* DEVICE [n_rows] parent of every row in its request's tree, a row
+                                  before it, or -1: the cached tokens; NULL: the row before it */
+  const int32_t* coord_base;   /* DEVICE [B] coordinate of a request's row 0, or NULL: cached_len */
+  int32_t* status;             /* DEVICE [1] CS_PLAN_* flags are added here; the caller clears it */
+} cs_page_plan;
+
+enum {
+  CS_PLAN_BAD_LENGTH = 1,      /* a length, page count or free_head is negative, the pages held do not
+                                  hold the cached tokens, or a token index would reach 2^31 */
+  CS_PLAN_TABLE_FULL = 2,      /* a request needs more than max_blocks pages */
+  CS_PLAN_POOL_FULL = 4,       /* the free pages do not suffice */
+  CS_PLAN_TOO_MANY_ROWS = 8,   /* more than n_rows rows */
+  CS_PLAN_MASK_TOO_SMALL = 16, /* a request has more than 64 x mask_words rows */
+  CS_PLAN_BAD_PARENT = 32,     /* a parent is neither -1 nor a row before its child: taken for -1 */
+  CS_PLAN_BAD_PAGE = 64        /* a page taken from the free list is outside the pool: used as it is,
+                                  and left out by the other calls */
+};
+
+/* ---------------------------------------------------------------------------
+ * batch_plan_pages -- block tables, slots, coordinates and tree masks of a
+ * step, from the requests' lengths.
+ *
+ * Request b needs ceil((cached_len[b] + new_len[b]) / P) pages; what it lacks is
+ * taken from the free list, request by request in order, and put behind the
+ * pages it holds.  Written: batch->row_start, the new entries of
+ * batch->block_table (the others are left as they are), batch->slot,
+ * batch->coords (all three axes coord_base[b] + the row's depth, its number of
+ * ancestors), batch->tree_mask when it is not NULL (the row itself and its
+ * ancestors), n_blocks_out, free_head_out and, when something is wrong, status.
+ * Rows behind the last request's get slot -1; their coordinates and masks are
+ * left as they are.  A step that cannot be planned (the flags up to
+ * CS_PLAN_MASK_TOO_SMALL) takes nothing: row_start is zero throughout, so that
+ * the step's other calls find no rows, every slot is -1, and n_blocks_out and
+ * free_head_out repeat what was there.
+ *
+ *   page      geometry of a page (only n_tokens matters beside its checks)
+ *   n_pages   pages of the pool
+ *   batch     every pointer but tree_mask is required (where B, n_rows are not 0)
+ * Errors: CS_ERR_INVALID_ARGUMENT for a bad geometry, size or NULL pointer, or
+ * for plan->parent without batch->tree_mask.                               */
+cs_status batch_plan_pages(const cs_geometry* page, int64_t n_pages, const cs_batch* batch,
+                           const cs_page_plan* plan, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * qk_norm_rope_append -- RMS norm of every query and key head, the rotation of
+ * Eq. 2 at the row's coordinates, and the rows' keys and values put into their
+ * pages, in one pass over the rows.
+ *
+ *   y = x / sqrt(mean_d x_d^2 + eps) * weight      (norm, per head)
+ *   (y_i, y_{i+D/2}) turned by coords[axis(i)] * theta_i   (as everywhere here)
+ * Queries go to q_out, keys and (unchanged) values to slot[r] of the pool in
+ * `layer`.  Everything between is float32 (the angles float64), rounded once.
+ * Rows whose slot is outside the pool write no key and no value; a row's query
+ * is written whatever its slot is, for the rows below row_start[B] alone.
+ * A slot that two rows share gets one of them.
+ *
+ *   q, k, v            [n_rows][H_q | H_kv | H_kv][D]
+ *   q_weight, k_weight DEVICE [D], geometry.dtype, or NULL: that side is
+ *                      rotated without a norm
+ *   eps                finite, >= 0
+ *   q_out              [n_rows][H_q][D]; may be q itself (data and strides)
+ * Uses batch->row_start, slot and coords.
+ * Errors: CS_ERR_INVALID_ARGUMENT, CS_ERR_UNSUPPORTED (grid), CS_ERR_HIP.    */
+cs_status qk_norm_rope_append(const cs_geometry* page, const cs_page_pool* pool, int32_t layer,
+                              const cs_batch* batch, const cs_rows* q, const cs_rows* k, const cs_rows* v,
+                              const void* q_weight, const void* k_weight, float eps,
+                              const cs_rows* q_out, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * tree_attend_paged -- attention (Eq. 1) of the step's rows over their
+ * requests' pages, the step's own keys and values (already appended) included.
+ *
+ *   out[r][h] = softmax_j(q[r][h] . K[j] / sqrt(D)) V[j]
+ * over the keys j that row i of request b sees: every j < cached_len[b], and
+ * j = cached_len[b] + w for the rows w < new_len[b] that its mask names (w <= i
+ * without a mask).  lse[r][h] = log(sum_j exp(q . K[j] / sqrt(D))).  Softmax and
+ * accumulation run in float32; in bf16 the probabilities are rounded to bf16
+ * for the product with the values.  A row that sees no key gets 0 and -inf.
+ * Keys and values that a row does not see do not matter, infinities and NaN
+ * included.  Rows of out and lse at row_start[B] and behind it are left as
+ * they are.  Results do not depend on timing.
+ *
+ *   q, out     [n_rows][H_q][D]; out may be q itself (data and strides)
+ *   lse        DEVICE float32 [n_rows][H_q], or NULL
+ *   workspace  DEVICE, >= tree_attend_paged_workspace() of the same geometry
+ *              and n_rows; no initial contents needed; calls that overlap need
+ *              one each
+ * Uses batch->cached_len, row_start, block_table and tree_mask.
+ * Errors: CS_ERR_INVALID_ARGUMENT, CS_ERR_WORKSPACE_TOO_SMALL,
+ * CS_ERR_UNSUPPORTED (grid), CS_ERR_HIP.                                    */
+cs_status tree_attend_paged_workspace(const cs_geometry* page, const cs_batch* batch, size_t* bytes);
+cs_status tree_attend_paged(const cs_geometry* page, const cs_page_pool* pool, int32_t layer,
+                            const cs_batch* batch, const cs_rows* q, const cs_rows* out, float* lse,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * tree_commit_paged -- the rows of an accepted path become cached tokens.
+ *
+ * For every request b and i < n_accepted[b], row accepted[b][i] of the request
+ * (its token cached_len[b] + accepted[b][i]) moves to token cached_len[b] + i,
+ * keys and values, in the layers [layer_begin, layer_end), and cached_len_out[b]
+ * = cached_len[b] + n_accepted[b].  The keys' rotation stays: a row's coordinate
+ * is its depth's, which is i.  A path's rows ascend; it ends before the first
+ * entry that does not ascend or is not a row of the request (then
+ * cached_len_out counts the entries before it).  Every other token is left as
+ * it is.  Requests that share a page they write race.
+ *
+ *   accepted        DEVICE int32 [B][max_accept]
+ *   n_accepted      DEVICE int32 [B]
+ *   cached_len_out  DEVICE int32 [B], not batch->cached_len; or NULL
+ * Uses batch->cached_len, row_start and block_table.
+ * Errors: CS_ERR_INVALID_ARGUMENT, CS_ERR_UNSUPPORTED (grid), CS_ERR_HIP.    */
+cs_status tree_commit_paged(const cs_geometry* page, const cs_page_pool* pool, int32_t layer_begin,
+                            int32_t layer_end, const cs_batch* batch, const int32_t* accepted,
+                            int32_t max_accept, const int32_t* n_accepted, int32_t* cached_len_out,
+                            void* stream);
+
 /* Thread-local text describing the last non-OK status on this thread. */
 const char* cs_last_error(void);
 

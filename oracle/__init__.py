@@ -18,8 +18,9 @@ Modules
   select     top-rho selection over later-chunk tokens (Section 2, after Eq. 5)
   attention  scatter of fresh K/V rows, then causal GQA softmax attention (Eq. 1)
   compose    the stages chained in the paper's order
+  batch      plan, norm and rotation, attention and commit of requests over a pool of pages
 
 Every function here is pinned by ``tests/test_oracle_*.py`` against closed
 forms, invariants, library routines or brute force; none is "parity unpinned".
 """
-from . import bf16, rope, rebase, score, select, attention, compose, inputs, policies  # noqa: F401
+from . import bf16, rope, rebase, score, select, attention, compose, inputs, policies, batch  # noqa: F401

@@ -37,6 +37,33 @@ class Geometry(ctypes.Structure):
                 ("chunk_start", ctypes.POINTER(ctypes.c_int64))]
 
 
+class Rows(ctypes.Structure):
+    """cs_rows: where the heads of rows lie (strides in elements).  Rows.of(t) describes a tensor
+    [n_rows, heads, D] whose last dimension is contiguous; the calls take such a tensor too."""
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+    @classmethod
+    def of(cls, t):
+        if t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] != 1):
+            raise ValueError("rows are a tensor [n_rows, heads, D] with a contiguous last dimension")
+        return cls(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+class _PagePool(ctypes.Structure):
+    _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("n_pages", ctypes.c_int64)]
+
+
+class _Batch(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_requests", "n_rows", "max_blocks", "mask_words", "max_rows")] + [
+        (n, ctypes.c_void_p) for n in ("cached_len", "row_start", "block_table", "slot", "coords", "tree_mask")]
+
+
+class _PagePlan(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("new_len", "n_blocks", "n_blocks_out", "free_pages")] + [
+        ("n_free", ctypes.c_int32)] + [
+        (n, ctypes.c_void_p) for n in ("free_head", "free_head_out", "parent", "coord_base", "status")]
+
+
 _lib = None
 
 
@@ -70,6 +97,12 @@ def lib():
                                                      vp, sz, vp]
         L.selective_attend_scatter_rope_paged.argtypes = [G, vp, vp, i32, i32, vp, i64, vp, vp, vp, vp, vp,
                                                           vp, vp, sz, vp]
+        B, R = ctypes.POINTER(_Batch), ctypes.POINTER(Rows)
+        L.batch_plan_pages.argtypes = [G, i64, B, ctypes.POINTER(_PagePlan), vp]
+        L.qk_norm_rope_append.argtypes = [G, ctypes.POINTER(_PagePool), i32, B, R, R, R, vp, vp, ctypes.c_float, R, vp]
+        L.tree_attend_paged_workspace.argtypes = [G, B, ctypes.POINTER(sz)]
+        L.tree_attend_paged.argtypes = [G, ctypes.POINTER(_PagePool), i32, B, R, R, vp, vp, sz, vp]
+        L.tree_commit_paged.argtypes = [G, ctypes.POINTER(_PagePool), i32, i32, B, vp, i32, vp, vp, vp]
         L.cs_last_error.restype = ctypes.c_char_p
         L.cs_trace_enable.argtypes = [i32]
         L.cs_trace_only.argtypes = [ctypes.c_char_p]
@@ -84,6 +117,8 @@ def lib():
                      "compose_rebase_k_paged", "compose_rebase_k_tokens_paged", "score_deviation_topk_paged",
                      "compose_load_rebase_k_paged",
                      "selective_attend_scatter_paged", "selective_attend_scatter_rope_paged",
+                     "batch_plan_pages", "qk_norm_rope_append", "tree_attend_paged_workspace",
+                     "tree_attend_paged", "tree_commit_paged",
                      "cs_trace_enable", "cs_trace_only", "cs_trace_collect", "cs_trace_get"):
             getattr(L, name).restype = ctypes.c_int
         _lib = L
@@ -302,3 +337,136 @@ def selective_attend_scatter_rope_paged(geo, k_chunks, v_chunks, layer_begin, la
                                                      _ptr(q_pre), _ptr(k_pre), _ptr(v_fresh), _ptr(coords),
                                                      _ptr(out), _ptr(lse), _ptr(workspace), ws_bytes,
                                                      _stream(stream)))
+
+
+# ---------------------------------------------------------------- batches over a pool of pages
+def _array(t, name, dtype, shape, optional=False):
+    """Device address of a dense tensor of the given type and shape (None in the shape: any size)."""
+    if t is None:
+        if optional:
+            return None
+        raise ValueError(f"{name} is required")
+    if str(t.dtype) != "torch." + dtype or not t.is_contiguous() or t.dim() != len(shape) or any(
+            want is not None and have != want for have, want in zip(t.shape, shape)):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape}, got {t.dtype} {tuple(t.shape)}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be in device memory")
+    return t.data_ptr()
+
+
+_TORCH_DTYPE = {CS_F32: "float32", CS_BF16: "bfloat16"}
+
+
+class PagePool:
+    """cs_page_pool: the key and value pages, tensors [n_pages, L, H_kv, P, D] of the page geometry's type."""
+
+    def __init__(self, geo, k_pages, v_pages):
+        shape = (None, geo.g.n_layers, geo.g.n_kv_heads, geo.g.n_tokens, geo.g.head_dim)
+        self.tensors = (k_pages, v_pages)
+        self.c = _PagePool()
+        self.c.k_pages = _array(k_pages, "k_pages", _TORCH_DTYPE[geo.g.dtype], shape)
+        self.c.v_pages = _array(v_pages, "v_pages", _TORCH_DTYPE[geo.g.dtype], (k_pages.shape[0],) + shape[1:])
+        self.c.n_pages = k_pages.shape[0]
+
+
+class Batch:
+    """cs_batch: the arrays of a step.  int32 tensors cached_len [B], row_start [B + 1], block_table
+    [B, max_blocks], slot [n_rows], coords [n_rows, 3]; tree_mask int64 [n_rows, mask_words] or None."""
+
+    def __init__(self, cached_len, row_start, block_table, slot, coords, tree_mask=None, max_rows=0):
+        n, rows = cached_len.shape[0], slot.shape[0]
+        self.tensors = (cached_len, row_start, block_table, slot, coords, tree_mask)
+        c = self.c = _Batch()
+        c.n_requests, c.n_rows, c.max_blocks, c.max_rows = n, rows, block_table.shape[1], int(max_rows)
+        c.mask_words = 0 if tree_mask is None else tree_mask.shape[1]
+        c.cached_len = _array(cached_len, "cached_len", "int32", (n,))
+        c.row_start = _array(row_start, "row_start", "int32", (n + 1,))
+        c.block_table = _array(block_table, "block_table", "int32", (n, None))
+        c.slot = _array(slot, "slot", "int32", (rows,))
+        c.coords = _array(coords, "coords", "int32", (rows, 3))
+        c.tree_mask = _array(tree_mask, "tree_mask", "int64", (rows, None), optional=True)
+
+
+class PagePlan:
+    """cs_page_plan: what batch_plan_pages reads and writes beside the batch, int32 tensors new_len, n_blocks,
+    n_blocks_out, coord_base [B], free_pages [n_free], free_head, free_head_out, status [1], parent [n_rows]."""
+
+    def __init__(self, new_len, n_blocks, n_blocks_out, free_pages, free_head, free_head_out, status, parent=None,
+                 coord_base=None):
+        n = new_len.shape[0]
+        self.tensors = (new_len, n_blocks, n_blocks_out, free_pages, free_head, free_head_out, status, parent,
+                        coord_base)
+        c = self.c = _PagePlan()
+        c.new_len = _array(new_len, "new_len", "int32", (n,))
+        c.n_blocks = _array(n_blocks, "n_blocks", "int32", (n,))
+        c.n_blocks_out = _array(n_blocks_out, "n_blocks_out", "int32", (n,))
+        c.free_pages = _array(free_pages, "free_pages", "int32", (None,))
+        c.n_free = free_pages.shape[0]
+        c.free_head = _array(free_head, "free_head", "int32", (1,))
+        c.free_head_out = _array(free_head_out, "free_head_out", "int32", (1,))
+        c.status = _array(status, "status", "int32", (1,))
+        c.parent = _array(parent, "parent", "int32", (None,), optional=True)
+        c.coord_base = _array(coord_base, "coord_base", "int32", (n,), optional=True)
+        self.n_requests, self.n_parents = n, None if parent is None else parent.shape[0]
+
+
+def _row_arg(t, name, geo, batch, heads):
+    """A Rows, or a tensor that is checked and described."""
+    if isinstance(t, Rows):
+        return t
+    if str(t.dtype) != "torch." + _TORCH_DTYPE[geo.g.dtype] or not t.is_cuda or t.dim() != 3 or (
+            t.shape[0] < batch.c.n_rows or t.shape[1] != heads or t.shape[2] != geo.g.head_dim):
+        raise ValueError(f"{name} must be a {_TORCH_DTYPE[geo.g.dtype]} device tensor [{batch.c.n_rows}, {heads}, "
+                         f"{geo.g.head_dim}], got {t.dtype} {tuple(t.shape)}")
+    return Rows.of(t)
+
+
+def batch_plan_pages(geo, n_pages, batch, plan, stream=None):
+    """Block tables, slots, coordinates and tree masks of the step, into the batch's arrays and the plan's outputs."""
+    if plan.n_requests != batch.c.n_requests or plan.n_parents not in (None, batch.c.n_rows):
+        raise ValueError("the plan's tensors are of another batch")
+    _check(lib().batch_plan_pages(geo.ref, int(n_pages), ctypes.byref(batch.c), ctypes.byref(plan.c),
+                                  _stream(stream)))
+
+
+def qk_norm_rope_append(geo, pool, layer, batch, q, k, v, q_out, q_weight=None, k_weight=None, eps=1e-6,
+                        stream=None):
+    """Norm and rotation of the step's queries (to q_out) and keys; keys and values to their slots in `layer`."""
+    hq, hkv = geo.g.n_q_heads, geo.g.n_kv_heads
+    w = [_array(x, "a weight", _TORCH_DTYPE[geo.g.dtype], (geo.g.head_dim,), optional=True)
+         for x in (q_weight, k_weight)]
+    _check(lib().qk_norm_rope_append(geo.ref, ctypes.byref(pool.c), int(layer), ctypes.byref(batch.c),
+                                     ctypes.byref(_row_arg(q, "q", geo, batch, hq)),
+                                     ctypes.byref(_row_arg(k, "k", geo, batch, hkv)),
+                                     ctypes.byref(_row_arg(v, "v", geo, batch, hkv)), w[0], w[1], float(eps),
+                                     ctypes.byref(_row_arg(q_out, "q_out", geo, batch, hq)), _stream(stream)))
+
+
+def tree_attend_paged_workspace(geo, batch):
+    n = ctypes.c_size_t(0)
+    _check(lib().tree_attend_paged_workspace(geo.ref, ctypes.byref(batch.c), ctypes.byref(n)))
+    return n.value
+
+
+def tree_attend_paged(geo, pool, layer, batch, q, out, lse=None, workspace=None, stream=None):
+    """Attention of the step's rows over their requests' pages; lse: float32 [n_rows, H_q] or None."""
+    hq = geo.g.n_q_heads
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    if lse is not None and lse.shape[0] < batch.c.n_rows:
+        raise ValueError("lse has fewer rows than the batch")
+    _check(lib().tree_attend_paged(geo.ref, ctypes.byref(pool.c), int(layer), ctypes.byref(batch.c),
+                                   ctypes.byref(_row_arg(q, "q", geo, batch, hq)),
+                                   ctypes.byref(_row_arg(out, "out", geo, batch, hq)),
+                                   _array(lse, "lse", "float32", (None, hq), optional=True), _ptr(workspace),
+                                   ws_bytes, _stream(stream)))
+
+
+def tree_commit_paged(geo, pool, layer_begin, layer_end, batch, accepted, n_accepted, cached_len_out=None,
+                      stream=None):
+    """Moves the rows of accepted int32 [B, max_accept] (n_accepted [B] of them) behind the cached tokens."""
+    n = batch.c.n_requests
+    _check(lib().tree_commit_paged(geo.ref, ctypes.byref(pool.c), int(layer_begin), int(layer_end),
+                                   ctypes.byref(batch.c), _array(accepted, "accepted", "int32", (n, None)),
+                                   accepted.shape[1], _array(n_accepted, "n_accepted", "int32", (n,)),
+                                   _array(cached_len_out, "cached_len_out", "int32", (n,), optional=True),
+                                   _stream(stream)))
