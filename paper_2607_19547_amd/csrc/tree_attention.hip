@@ -3,6 +3,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "batch.h"
 
@@ -121,40 +122,752 @@ __global__ __launch_bounds__(kAnyThreads) void tree_attend_any(const TreeArgs a)
   if (a.lse && tid == 0) a.lse[(int64_t)r * a.Hq + h] = any ? m + logf(l) : -INFINITY;
 }
 
-size_t tree_attend_workspace(const Geo&, const cs_batch&) { return 0; }
+// ============================================================== matrix-instruction path
+// Head dims that fill whole 64-byte pieces of a row (bf16: multiples of 32,
+// float32: of 16, see tree_instance), pages of a multiple of 16 tokens.
+//
+// A unit is one request, one KV head and a row tile of 16 NR query vectors
+// (its rows x the G query heads that share the KV head).  A wavefront takes a
+// tile of kTile keys: with the keys as the rows of the matrix instruction,
+//   S^T = K Q^T       each lane holds 4 or 8 scores of ONE query vector
+//   O^T += V^T P^T    with those scores' probabilities as the operand as they are
+// since the order of the keys inside a product is free: lane group g = lane / 16
+// holds keys 4 g .. 4 g + 3 of each 16, and loads those rows of V.  K and V go
+// from memory straight into the operands' registers (a row's pieces of 16
+// bytes belong to one lane); only V's 16-bit elements have to be paired by key,
+// four byte permutes per product.  No LDS and no barrier in the loop, so a
+// wavefront's loads run ahead of its arithmetic: while a tile is worked on, the
+// next one's keys are in flight from the end of its scores on, and its values
+// from the end of its products on.
+//
+// Bound by memory for few rows (every key and value is read once per row tile).
+// The work, in key tiles over all units, is cut into equal runs, one for each
+// workgroup, whatever the requests' lengths: a run ends inside a unit or spans
+// several.  A unit that one workgroup has whole is finished there; of the
+// others each piece leaves a partial (O, max, sum), and tree_combine merges
+// them in key order, so results do not depend on timing.  Every workgroup
+// finds its run from the lengths alone (one load and a prefix sum).
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+// The running maximum may grow by 2^5 before the accumulators are rescaled:
+// probabilities stay far inside the range of both types.
+constexpr float kRescaleLog2 = 5.f;
+
+struct SplitArgs {
+  TreeArgs t;
+  float* part;      // [2 workgroups][row tile][D] unnormalised partial outputs
+  float* part_ml;   // [2 workgroups][row tile][2] their maximum (log2 units) and sum
+  int min_tiles;    // key tiles of a run at least
+  int row_bits;     // a row tile has 2^row_bits query vectors
+  int tile_bits;    // a key tile has 2^tile_bits keys
+  int run_bits;     // 2^run_bits runs at most
+  FastDiv group;    // division by G
+};
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  return (int64_t)(((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32) | (uint32_t)uniform((int)x));
+}
+__device__ __forceinline__ Request uniform(Request q) {
+  q.r0 = uniform(q.r0);
+  q.n = uniform(q.n);
+  q.cached = uniform(q.cached);
+  q.len = uniform(q.len);
+  return q;
+}
+__device__ __forceinline__ void unit_sizes(const SplitArgs& a, const Request& q, int* nrt, int* ntile) {
+  *nrt = (int)(((int64_t)q.n * a.t.G + (1 << a.row_bits) - 1) >> a.row_bits);
+  *ntile = max((int)(((int64_t)q.len + (1 << a.tile_bits) - 1) >> a.tile_bits), 1);
+}
+// Unit of the key tile at `off` of a request, and the tile in it (a quotient
+// below 2^31 of numbers below 2^53).
+__device__ __forceinline__ int unit_at(int64_t off, int ntile, int* tile) {
+  int u = (int)((double)off / (double)ntile);
+  if ((int64_t)u * ntile > off) --u;
+  *tile = (int)(off - (int64_t)u * ntile);
+  return u;
+}
+// Key tiles of a run: the same for all, so that run w is [w x len, (w + 1) x len).
+__device__ __forceinline__ int64_t run_length(const SplitArgs& a, int64_t total) {
+  return max((int64_t)a.min_tiles, (total + (1 << a.run_bits) - 1) >> a.run_bits);
+}
+
+struct RunShared {
+  int64_t red[kWaves];
+  int64_t off;
+  int b;
+};
+struct Run {
+  int64_t begin, end, total, off;  // key tiles [begin, end) of `total`; begin is tile `off` of request b
+  int b;
+};
+// Run w; false (for the whole workgroup) where there is none.
+__device__ __forceinline__ bool find_run(const SplitArgs& a, int w, RunShared& sh, Run* run) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int per = (a.t.B + kThreads - 1) / kThreads;
+  auto tiles = [&](int b) -> int64_t {
+    int nrt, ntile;
+    unit_sizes(a, load_request(a.t, b), &nrt, &ntile);
+    return (int64_t)a.t.Hkv * nrt * ntile;
+  };
+  int64_t sum = 0;
+  for (int j = 0; j < per; ++j) {
+    const int b = tid * per + j;
+    if (b < a.t.B) sum += tiles(b);
+  }
+  const int64_t inc = wave_scan64(sum);
+  if (lane == 63) sh.red[wave] = inc;
+  __syncthreads();
+  int64_t before = 0, total = 0;
+#pragma unroll
+  for (int x = 0; x < kWaves; ++x) {
+    before += x < wave ? sh.red[x] : 0;
+    total += sh.red[x];
+  }
+  total = uniform(total);
+  const int64_t len = run_length(a, total), begin = w * len;
+  if (begin >= total) return false;
+  int64_t at = before + inc - sum;
+  if (begin >= at && begin < at + sum) {
+    int b = tid * per;
+    for (;; ++b) {
+      const int64_t x = tiles(b);
+      if (begin < at + x) break;
+      at += x;
+    }
+    sh.b = b;
+    sh.off = begin - at;
+  }
+  __syncthreads();
+  run->begin = begin;
+  run->end = min(begin + len, total);
+  run->total = total;
+  run->off = uniform(sh.off);
+  run->b = uniform(sh.b);
+  return true;
+}
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const char* base, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00020000);
+}
+template <int BYTES>
+struct Words {
+  uint32_t w[BYTES / 4];
+};
+template <int BYTES>
+__device__ __forceinline__ Words<BYTES> load_words(__amdgpu_buffer_rsrc_t r, int off) {
+  Words<BYTES> o;
+  if constexpr (BYTES == 16) {
+    const auto v = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0);
+    for (int i = 0; i < 4; ++i) o.w[i] = v[i];
+  } else if constexpr (BYTES == 12) {
+    const auto v = __builtin_amdgcn_raw_buffer_load_b96(r, off, 0, 0);
+    for (int i = 0; i < 3; ++i) o.w[i] = v[i];
+  } else if constexpr (BYTES == 8) {
+    const auto v = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0);
+    for (int i = 0; i < 2; ++i) o.w[i] = v[i];
+  } else {
+    o.w[0] = __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0);
+  }
+  return o;
+}
+
+// Over the four lanes that hold one query vector: l, l ^ 16, l ^ 32, l ^ 48.
+__device__ __forceinline__ float group_max(float x) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float group_sum(float x) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+template <typename E, int D, int NR>
+__global__ __launch_bounds__(kThreads, NR * D * sizeof(E) <= 256 ? 2 : 1) void tree_attend(const SplitArgs a) {
+  constexpr bool kBf16 = sizeof(E) == 2;
+  constexpr int SUB = kBf16 ? 2 : 1;             // 16-key pieces of a tile
+  constexpr int KT = 16 * SUB;
+  constexpr int kRowB = D * (int)sizeof(E);
+  constexpr int KS = kRowB / 64;                 // 64-byte pieces of a row
+  constexpr int NB = kRowB > 256 ? kRowB / 256 : 1;  // blocks of a row that 16 lanes load
+  constexpr int VB = kRowB / 16 / NB;            // bytes of a V row a lane loads per block
+  constexpr int VW = VB / (int)sizeof(E);
+  constexpr int NO = NB * VW;                    // output tiles: 16 elements x 16 query vectors
+  constexpr int RT = 16 * NR;
+  constexpr int NS = 4 * SUB;                    // scores of a lane per 16 query vectors
+  constexpr int kPad = D + 4;
+  static_assert(KS * 64 == kRowB && NO * 16 == D && VB % 4 == 0, "head dim");
+
+  __shared__ RunShared sh;
+  __shared__ float s_o[kWaves * 16 * kPad];
+  __shared__ float s_m[kWaves][16], s_l[kWaves][16];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int ln = lane & 15, lg = lane >> 4;
+  Run run;
+  if (!find_run(a, blockIdx.x, sh, &run)) return;
+  const TreeArgs& t = a.t;
+  int64_t left = run.end - run.begin, off = run.off;
+  int b = run.b;
+  const float sc = t.scale * kLog2e;
+  bool first_seg = true;
+
+  while (left > 0) {
+    const Request q = uniform(load_request(t, b));
+    int nrt, ntile;
+    unit_sizes(a, q, &nrt, &ntile);
+    nrt = uniform(nrt);
+    ntile = uniform(ntile);
+    if (off >= (int64_t)t.Hkv * nrt * ntile) {  // behind this request's units
+      off = 0;
+      ++b;
+      continue;
+    }
+    int t0;
+    const int u = uniform(unit_at(off, ntile, &t0));
+    t0 = uniform(t0);
+    const int seg = (int)min(left, (int64_t)(ntile - t0));
+    const int h = uniform(u / nrt), rt = u - h * nrt;
+    const bool whole = seg == ntile;
+    // rows see no key behind their own without a mask, so later tiles are left out
+    const int i_last = a.group.div(min(rt * RT + RT - 1, q.n * t.G - 1));
+    const int key_end = t.mask ? q.len : min(q.len, q.cached + i_last + 1);
+    const int t_end = min(t0 + seg, (key_end + KT - 1) / KT);
+
+    Words<16> qf[NR][KS];
+    int row[NR];  // the lane's row in the request, per 16 query vectors
+#pragma unroll
+    for (int x = 0; x < NR; ++x) {
+      const int qv = rt * RT + 16 * x + ln;
+      const bool valid = qv < q.n * t.G;
+      const int i = valid ? a.group.div(qv) : q.n - 1;
+      row[x] = i;
+      const char* qp = (const char*)t.q + ((int64_t)(q.r0 + i) * t.q_row + (h * t.G + (valid ? qv - i * t.G : 0)) * t.q_head) * (int)sizeof(E);
+#pragma unroll
+      for (int k = 0; k < KS; ++k) qf[x][k] = *(const Words<16>*)(qp + 64 * k + 16 * lg);
+    }
+
+    const int32_t* table = t.table + (int64_t)b * t.max_blocks;
+    const int64_t plane = ((int64_t)t.layer * t.Hkv + h) * t.page.d * kRowB;
+    Words<16> kf[SUB][KS];
+    Words<VB> vf[SUB * 4][NB];
+    bool have[SUB];  // the 16 keys lie in a page of the pool
+    // Where the 16-key pieces of a tile lie: 16 rows of a page (pages are
+    // multiples of 16 tokens), as many of them as the request has; none behind
+    // the request's or the run's end.  The page numbers come through the scalar
+    // cache, a tile ahead of the loads that need them, so that nothing waits
+    // for the values in flight.
+    typedef const __attribute__((address_space(4))) int32_t* scalar_ptr;
+    const scalar_ptr pages = (scalar_ptr)(uint64_t)table;
+    int64_t at[SUB];
+    int bytes[SUB], page[SUB];
+    bool ok[SUB];
+    auto fetch_pages = [&](int tile) {
+#pragma unroll
+      for (int s = 0; s < SUB; ++s) {
+        const int key = min(tile, t_end - 1) * KT + 16 * s;
+        page[s] = pages[t.page.div(min(key, q.len - 1))];
+      }
+    };
+    auto places = [&](int tile) {
+#pragma unroll
+      for (int s = 0; s < SUB; ++s) {
+        const int key = tile * KT + 16 * s;
+        ok[s] = tile < t_end && key < q.len && page[s] >= 0 && page[s] < t.pool.n_pages;
+        at[s] = ok[s] ? page[s] * t.pool.page_bytes + plane + (int64_t)(key - t.page.div(key) * t.page.d) * kRowB : 0;
+        bytes[s] = ok[s] ? min(q.len - key, 16) * kRowB : 0;
+      }
+    };
+    auto load_k = [&]() {
+#pragma unroll
+      for (int s = 0; s < SUB; ++s) {
+        const auto r = rows_rsrc(t.pool.k + at[s], bytes[s]);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) kf[s][k] = load_words<16>(r, ln * kRowB + 64 * k + 16 * lg);
+      }
+    };
+    auto load_v = [&]() {
+#pragma unroll
+      for (int s = 0; s < SUB; ++s) {
+        const auto r = rows_rsrc(t.pool.v + at[s], bytes[s]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int n = 0; n < NB; ++n) vf[4 * s + i][n] = load_words<VB>(r, (4 * lg + i) * kRowB + n * 16 * VB + VB * ln);
+      }
+    };
+
+    f32x4 o[NR][NO];
+    float m[NR], l[NR];
+    bool seen[NR];  // some key was visible
+#pragma unroll
+    for (int x = 0; x < NR; ++x) {
+      m[x] = -INFINITY;
+      l[x] = 0.f;
+      seen[x] = false;
+#pragma unroll
+      for (int e = 0; e < NO; ++e) o[x][e] = f32x4{};
+    }
+
+    int tile = t0 + wave;
+    if (tile < t_end && q.len > 0) {
+      fetch_pages(tile);
+      places(tile);
+      load_k();
+      load_v();
+      fetch_pages(tile + kWaves);
+    }
+    auto step = [&](auto masked) {
+      constexpr bool kMasked = decltype(masked)::value;
+      const int key0 = tile * KT;
+      f32x4 s[NR][SUB];
+#pragma unroll
+      for (int x = 0; x < NR; ++x)
+#pragma unroll
+        for (int y = 0; y < SUB; ++y) {
+          s[x][y] = f32x4{};
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            if constexpr (kBf16) {
+              s[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[y][k]),
+                                                                __builtin_bit_cast(bf16x8, qf[x][k]), s[x][y], 0, 0, 0);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                s[x][y] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[y][k].w[e]),
+                                                               __uint_as_float(qf[x][k].w[e]), s[x][y], 0, 0, 0);
+            }
+          }
+        }
+#pragma unroll
+      for (int y = 0; y < SUB; ++y) have[y] = ok[y];
+      places(tile + kWaves);
+      load_k();
+      fetch_pages(tile + 2 * kWaves);
+
+      uint32_t vis[NR];  // bit of key 16 y + 4 lg + i at 16 y + 4 lg + i
+      if constexpr (kMasked) {
+        uint32_t there = 0;  // keys of the request that lie in the pool
+#pragma unroll
+        for (int y = 0; y < SUB; ++y) {
+          const int n = min(max(q.len - key0 - 16 * y, 0), 16);
+          if (have[y]) there |= ((1u << n) - 1) << (16 * y);
+        }
+        const int w0 = key0 - q.cached;  // new row of the tile's first key
+#pragma unroll
+        for (int x = 0; x < NR; ++x) {
+          uint64_t bits = 0;  // visible rows from max(w0, 0) on
+          const int w = max(w0, 0);
+          if (t.mask) {
+            const unsigned long long* mk = t.mask + (int64_t)(q.r0 + row[x]) * t.words;
+            const int j = w >> 6, sft = w & 63;
+            if (w0 + KT > 0 && j < t.words) bits = mk[j] >> sft;
+            if (w0 + KT > 0 && sft && j + 1 < t.words) bits |= mk[j + 1] << (64 - sft);
+          } else {
+            const int n = row[x] - w + 1;
+            bits = n >= 64 ? ~0ull : n > 0 ? (1ull << n) - 1 : 0ull;
+          }
+          if (w0 < 0) bits = -w0 >= 64 ? ~0ull : bits << -w0 | ((1ull << -w0) - 1);
+          vis[x] = (uint32_t)bits & there;
+          seen[x] = seen[x] || vis[x];
+        }
+      } else {
+        bool some = false;
+#pragma unroll
+        for (int y = 0; y < SUB; ++y) some = some || have[y];
+#pragma unroll
+        for (int x = 0; x < NR; ++x) seen[x] = seen[x] || some;
+      }
+
+      float p[NR][NS];
+#pragma unroll
+      for (int x = 0; x < NR; ++x) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int y = 0; y < SUB; ++y)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            // (keys in no page of the pool: not seen)
+            float v = kMasked ? s[x][y][i] * sc : fmaf(s[x][y][i], sc, have[y] ? 0.f : -INFINITY);
+            if constexpr (kMasked) v = (vis[x] >> (16 * y + 4 * lg + i)) & 1 ? v : -INFINITY;
+            p[x][4 * y + i] = v;
+            mx = fmaxf(mx, v);
+          }
+        mx = group_max(mx);
+        const bool grow = mx > m[x] + kRescaleLog2;
+        if (__ballot(grow)) {
+          const float m_new = grow ? mx : m[x];
+          const float alpha = grow ? __builtin_amdgcn_exp2f(m[x] - m_new) : 1.f;
+          l[x] *= alpha;
+#pragma unroll
+          for (int e = 0; e < NO; ++e) o[x][e] *= alpha;
+          m[x] = m_new;
+        }
+        const float ref = m[x] == -INFINITY ? 0.f : m[x];
+#pragma unroll
+        for (int j = 0; j < NS; ++j) {
+          p[x][j] = __builtin_amdgcn_exp2f(p[x][j] - ref);
+          l[x] += p[x][j];
+        }
+      }
+
+      // Values that are not finite must not reach rows that do not see them
+      // (0 x inf): rare, and only among the step's own rows.
+      uint32_t odd = 0;  // the exponents' carries: all ones
+      if constexpr (kMasked) {
+#pragma unroll
+        for (int j = 0; j < SUB * 4; ++j)
+#pragma unroll
+          for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int w = 0; w < VB / 4; ++w) {
+              const uint32_t v = vf[j][n].w[w];
+              odd |= kBf16 ? (v & 0x7f807f80u) + 0x00800080u : (v & 0x7f800000u) + 0x00800000u;
+            }
+      }
+      auto pv = [&](auto value, auto weight, auto add) {
+        // value(j, n, w): word w of key j's block n; weight(x, j): of query vector and key
+        if constexpr (kBf16) {
+          bf16x8 pb[NR];
+#pragma unroll
+          for (int x = 0; x < NR; ++x)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) pb[x][j] = (__bf16)weight(x, j);
+#pragma unroll
+          for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int e = 0; e < VW; ++e) {
+              u32x4 va;
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                va[j] = __builtin_amdgcn_perm(value(2 * j + 1, n, e / 2), value(2 * j, n, e / 2), e & 1 ? 0x07060302 : 0x05040100);
+#pragma unroll
+              for (int x = 0; x < NR; ++x)
+                add(x, n * VW + e, [&](f32x4 c) {
+                  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va), pb[x], c, 0, 0, 0);
+                });
+            }
+        } else {
+#pragma unroll
+          for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int e = 0; e < VW; ++e)
+#pragma unroll
+              for (int x = 0; x < NR; ++x)
+                add(x, n * VW + e, [&](f32x4 c) {
+#pragma unroll
+                  for (int j = 0; j < 4; ++j)
+                    c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(value(j, n, e)), weight(x, j), c, 0, 0, 0);
+                  return c;
+                });
+        }
+      };
+      if (kMasked && __ballot(odd & (kBf16 ? 0x80008000u : 0x80000000u))) {
+        // How many values of +inf (or NaN), and of -inf (or NaN), each output
+        // element gets from keys that its row sees; those give it the infinity,
+        // both of them NaN.  The values themselves become zero.
+#pragma unroll 1
+        for (int sign = 0; sign < 2; ++sign) {
+          auto flag16 = [&](uint32_t v) -> uint32_t {  // 1.0 in bf16 where the element counts
+            const bool nan = (v & 0x7f80u) == 0x7f80u && (v & 0x7fu);
+            return nan || (v & 0xffffu) == (sign ? 0xff80u : 0x7f80u) ? 0x3f80u : 0u;
+          };
+          auto flag = [&](uint32_t v) -> uint32_t {
+            if constexpr (kBf16) return flag16(v) | flag16(v >> 16) << 16;
+            const bool nan = (v & 0x7f800000u) == 0x7f800000u && (v & 0x7fffffu);
+            return nan || v == (sign ? 0xff800000u : 0x7f800000u) ? 0x3f800000u : 0u;
+          };
+          pv([&](int j, int n, int w) { return flag(vf[j][n].w[w]); },
+             [&](int x, int j) { return (vis[x] >> (16 * (j >> 2) + 4 * lg + (j & 3))) & 1 ? 1.f : 0.f; },
+             [&](int x, int e, auto mul) {
+               const f32x4 c = mul(f32x4{});
+#pragma unroll
+               for (int i = 0; i < 4; ++i)
+                 if (c[i] > 0.f) o[x][e][i] += sign ? -INFINITY : INFINITY;
+             });
+        }
+#pragma unroll
+        for (int j = 0; j < SUB * 4; ++j)
+#pragma unroll
+          for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int w = 0; w < VB / 4; ++w) {
+              uint32_t& v = vf[j][n].w[w];
+              if (kBf16) {
+                if ((v & 0x7f80u) == 0x7f80u) v &= 0xffff0000u;
+                if ((v & 0x7f800000u) == 0x7f800000u) v &= 0xffffu;
+              } else if ((v & 0x7f800000u) == 0x7f800000u) {
+                v = 0;
+              }
+            }
+      }
+      pv([&](int j, int n, int w) { return vf[j][n].w[w]; }, [&](int x, int j) { return p[x][j]; },
+         [&](int x, int e, auto mul) { o[x][e] = mul(o[x][e]); });
+      load_v();
+    };
+    // tiles whose keys every row sees, then those with the step's own rows
+    const int t_full = min(t_end, min(q.cached, q.len) / KT);
+    for (; tile < t_full; tile += kWaves) step(std::false_type{});
+    for (; tile < t_end; tile += kWaves) step(std::true_type{});
+
+    // The wavefronts' results, 16 query vectors at a time, merged through LDS:
+    // O = sum_w 2^(m_w - M) O_w.  A maximum of -inf has weight 0; where all are
+    // -inf the sum is 0 (no key seen) or NaN (only scores of -inf seen).
+    const int slot = 2 * blockIdx.x + (first_seg ? 0 : 1);
+#pragma unroll
+    for (int x = 0; x < NR; ++x) {
+      float lt = group_sum(l[x]);
+      if (seen[x] && m[x] == -INFINITY) lt = __builtin_nanf("");
+      __syncthreads();  // the previous 16 have been read
+      if (lg == 0) {
+        s_m[wave][ln] = m[x];
+        s_l[wave][ln] = lt;
+      }
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float* d = s_o + (wave * 16 + ln) * kPad + n * 16 * VW + VW * (4 * lg + i);
+#pragma unroll
+          for (int e = 0; e < VW; ++e) d[e] = o[x][n * VW + e][i];
+        }
+      __syncthreads();
+      const int r = tid >> 4, c = tid & 15;  // 16 threads a query vector, D / 16 elements each
+      const int qv = rt * RT + 16 * x + r;
+      if (qv < q.n * t.G) {
+        float M = -INFINITY, sum = 0.f, wgt[kWaves], acc[D / 16];
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_m[w][r]);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+          wgt[w] = s_m[w][r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[w][r] - M);
+          sum += s_m[w][r] == -INFINITY ? (M == -INFINITY ? s_l[w][r] : 0.f) : wgt[w] * s_l[w][r];
+        }
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e) acc[e] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w)
+          if (wgt[w] != 0.f)
+#pragma unroll
+            for (int e = 0; e < D / 16; ++e) acc[e] = fmaf(wgt[w], s_o[(w * 16 + r) * kPad + c * (D / 16) + e], acc[e]);
+        const int i = a.group.div(qv), head = h * t.G + qv - i * t.G;
+        if (whole) {
+          const float inv = sum == 0.f && M == -INFINITY ? 0.f : 1.f / sum;
+          E* op = (E*)t.out + (q.r0 + i) * t.o_row + head * t.o_head + c * (D / 16);
+          if constexpr (kBf16) {
+#pragma unroll
+            for (int e = 0; e < D / 16; e += 2) *(uint32_t*)(op + e) = pack_bf16x2(acc[e] * inv, acc[e + 1] * inv);
+          } else {
+#pragma unroll
+            for (int e = 0; e < D / 16; ++e) op[e] = acc[e] * inv;
+          }
+          if (t.lse && c == 0) t.lse[(int64_t)(q.r0 + i) * t.Hq + head] = (M + __log2f(sum)) * kLn2;
+        } else {
+          float* pp = a.part + ((int64_t)slot * RT + 16 * x + r) * D + c * (D / 16);
+#pragma unroll
+          for (int e = 0; e < D / 16; ++e) pp[e] = acc[e];
+          if (c == 0) {
+            float* ml = a.part_ml + ((int64_t)slot * RT + 16 * x + r) * 2;
+            ml[0] = M;
+            ml[1] = sum;
+          }
+        }
+      }
+    }
+    first_seg = false;
+    left -= seg;
+    off += seg;
+  }
+}
+
+// Merges the pieces of a unit that several workgroups worked on.  Workgroup
+// (w, y) looks at the border between runs w and w + 1: where it is the first
+// one inside a unit, it merges query vectors y, y + gridDim.y, ... of that unit.
+// 32 lanes hold one query vector's elements, the workgroup's groups of 32
+// take its pieces in turn.
+constexpr int kGroups = kThreads / 32;
+template <typename E, int D>
+__global__ __launch_bounds__(kThreads) void tree_combine(const SplitArgs a) {
+  __shared__ RunShared sh;
+  __shared__ float s_o[kGroups][D], s_m[kGroups], s_l[kGroups];
+  constexpr int C = D / 32 > 0 ? D / 32 : 1;  // elements a lane holds
+  const TreeArgs& t = a.t;
+  const int w1 = blockIdx.x + 1;
+  Run run;
+  if (!find_run(a, w1, sh, &run)) return;
+  const Request q = uniform(load_request(t, run.b));
+  int nrt, ntile, tile;
+  unit_sizes(a, q, &nrt, &ntile);
+  const int u = unit_at(run.off, ntile, &tile);
+  // only at the first border inside the unit
+  const int64_t len = run_length(a, run.total), unit0 = run.begin - tile, unit1 = unit0 + ntile, prev = run.begin - len;
+  if (tile == 0 || prev > unit0) return;
+  const int w0 = w1 - 1;
+  int w_last = w1;  // the run that holds the unit's last tile
+  while ((w_last + 1) * len < unit1) ++w_last;
+  const int pieces = w_last - w0 + 1;
+  const int h = u / nrt, rt = u - h * nrt;
+  const int grp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int r = blockIdx.y; r < 1 << a.row_bits && (rt << a.row_bits) + r < q.n * t.G; r += gridDim.y) {
+    float M = -INFINITY, sum = 0.f, acc[C];
+#pragma unroll
+    for (int e = 0; e < C; ++e) acc[e] = 0.f;
+    for (int x = grp; x < pieces; x += kGroups) {
+      // the first piece ends its run unless the run begins with the unit
+      const int64_t slot = 2 * (int64_t)(w0 + x) + (x == 0 && prev < unit0 ? 1 : 0);
+      const float* ml = a.part_ml + ((slot << a.row_bits) + r) * 2;
+      const float* pp = a.part + ((slot << a.row_bits) + r) * D + lane * C;
+      const float pm = ml[0], pl = ml[1];
+      float v[C];
+#pragma unroll
+      for (int e = 0; e < C; ++e) v[e] = lane * C + e < D ? pp[e] : 0.f;
+      if (pm == -INFINITY) {
+        if (M == -INFINITY) sum += pl;
+        continue;
+      }
+      const float mn = fmaxf(M, pm);
+      const float wa = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - mn), wb = __builtin_amdgcn_exp2f(pm - mn);
+      sum = M == -INFINITY ? wb * pl : sum * wa + wb * pl;
+#pragma unroll
+      for (int e = 0; e < C; ++e) acc[e] = M == -INFINITY ? wb * v[e] : fmaf(acc[e], wa, wb * v[e]);
+      M = mn;
+    }
+    __syncthreads();
+    if (lane == 0) {
+      s_m[grp] = M;
+      s_l[grp] = sum;
+    }
+#pragma unroll
+    for (int e = 0; e < C; ++e)
+      if (lane * C + e < D) s_o[grp][lane * C + e] = acc[e];
+    __syncthreads();
+    float Mt = -INFINITY, lt = 0.f;
+#pragma unroll
+    for (int x = 0; x < kGroups; ++x) Mt = fmaxf(Mt, s_m[x]);
+#pragma unroll
+    for (int x = 0; x < kGroups; ++x)
+      lt += s_m[x] == -INFINITY ? (Mt == -INFINITY ? s_l[x] : 0.f) : __builtin_amdgcn_exp2f(s_m[x] - Mt) * s_l[x];
+    const int qv = (rt << a.row_bits) + r, i = a.group.div(qv), head = h * t.G + qv - i * t.G;
+    const float inv = lt == 0.f && Mt == -INFINITY ? 0.f : 1.f / lt;
+    for (int d = threadIdx.x; d < D; d += kThreads) {
+      float v = 0.f;
+#pragma unroll
+      for (int x = 0; x < kGroups; ++x)
+        if (s_m[x] != -INFINITY) v = fmaf(__builtin_amdgcn_exp2f(s_m[x] - Mt), s_o[x][d], v);
+      put_elem((E*)t.out + (q.r0 + i) * t.o_row + head * t.o_head + d, v * inv);
+    }
+    if (t.lse && threadIdx.x == 0) t.lse[(int64_t)(q.r0 + i) * t.Hq + head] = (Mt + __log2f(lt)) * kLn2;
+  }
+}
+
+// ============================================================== launch
+constexpr int kRunBits = 9, kRuns = 1 << kRunBits;  // workgroups of the attention launch: two for each CU
+
+// Whether the matrix-instruction path has an instance: bf16 rows of 64 to 256
+// bytes, or 512; float32 rows of 64, 128, 256 or 512 bytes.
+static bool has_instance(const Geo& g) {
+  if (g.T % 16) return false;
+  if (g.dtype == CS_BF16) return g.D == 32 || g.D == 64 || g.D == 96 || g.D == 128 || g.D == 256;
+  return g.D == 16 || g.D == 32 || g.D == 64 || g.D == 128;
+}
+// Row tiles of 16, 32 or 64 query vectors: the smallest that holds the rows
+// that a request is expected to have.
+static int row_groups(const Geo& g, const cs_batch& b) {
+  const int64_t rows = b.max_rows > 0 ? b.max_rows : b.n_rows;
+  const int64_t qv = rows * g.G;
+  return qv <= 16 ? 1 : qv <= 32 ? 2 : 4;
+}
+
+size_t tree_attend_workspace(const Geo& g, const cs_batch& b) {
+  if (!has_instance(g)) return 0;
+  const size_t rows = 16 * (size_t)row_groups(g, b);
+  return 2 * (size_t)kRuns * rows * (g.D + 2) * sizeof(float) + 512;
+}
+
+template <typename E, int D, int NR>
+static void run_split(const SplitArgs& a, hipStream_t s) {
+  {
+    TraceScope tr("tree_attend", s);
+    CS_LAUNCH(tr, (tree_attend<E, D, NR>), dim3(kRuns), dim3(kThreads), 0, s, a);
+  }
+  TraceScope tr("tree_combine", s);
+  CS_LAUNCH(tr, (tree_combine<E, D>), dim3(kRuns - 1, 16), dim3(kThreads), 0, s, a);
+}
+template <typename E, int D>
+static void run_split(const SplitArgs& a, int nr, hipStream_t s) {
+  if (nr == 1) run_split<E, D, 1>(a, s);
+  else if (nr == 2) run_split<E, D, 2>(a, s);
+  else run_split<E, D, 4>(a, s);
+}
 
 cs_status launch_tree_attend(const Geo& g, const cs_page_pool& pool, int layer, const cs_batch& b, const cs_rows& q,
-                             const cs_rows& out, float* lse, void*, hipStream_t s, bool check_only) {
-  const cs_status st = check_grid(b.n_rows, g.Hq, 1, kAnyThreads, "tree attention");
-  if (st || check_only) return st;
-  TreeArgs a;
-  a.q = q.data;
-  a.out = out.data;
-  a.lse = lse;
-  a.q_row = q.row_stride;
-  a.q_head = q.head_stride;
-  a.o_row = out.row_stride;
-  a.o_head = out.head_stride;
-  a.cached = b.cached_len;
-  a.row_start = b.row_start;
-  a.table = b.block_table;
-  a.mask = (const unsigned long long*)b.tree_mask;
-  a.pool = pool_view(g, pool);
-  a.page = fast_div((int)g.T);
-  a.B = b.n_requests;
-  a.n_rows = b.n_rows;
-  a.max_blocks = b.max_blocks;
-  a.words = b.mask_words;
-  a.layer = layer;
-  a.Hq = g.Hq;
-  a.Hkv = g.Hkv;
-  a.G = g.G;
-  a.D = g.D;
-  a.scale = 1.f / sqrtf((float)g.D);
-  TraceScope tr("tree_attend_any", s);
-  const dim3 grid(b.n_rows, g.Hq);
-  if (g.dtype == CS_BF16) CS_LAUNCH(tr, tree_attend_any<uint16_t>, grid, dim3(kAnyThreads), 0, s, a);
-  else CS_LAUNCH(tr, tree_attend_any<float>, grid, dim3(kAnyThreads), 0, s, a);
+                             const cs_rows& out, float* lse, void* ws, hipStream_t s, bool check_only) {
+  SplitArgs a;
+  TreeArgs& t = a.t;
+  t.q = q.data;
+  t.out = out.data;
+  t.lse = lse;
+  t.q_row = q.row_stride;
+  t.q_head = q.head_stride;
+  t.o_row = out.row_stride;
+  t.o_head = out.head_stride;
+  t.cached = b.cached_len;
+  t.row_start = b.row_start;
+  t.table = b.block_table;
+  t.mask = (const unsigned long long*)b.tree_mask;
+  t.pool = pool_view(g, pool);
+  t.page = fast_div((int)g.T);
+  t.B = b.n_requests;
+  t.n_rows = b.n_rows;
+  t.max_blocks = b.max_blocks;
+  t.words = b.mask_words;
+  t.layer = layer;
+  t.Hq = g.Hq;
+  t.Hkv = g.Hkv;
+  t.G = g.G;
+  t.D = g.D;
+  t.scale = 1.f / sqrtf((float)g.D);
+  // 16-byte accesses of queries, 4-byte ones of outputs
+  const uint64_t low = (uint64_t)t.q | (uint64_t)((t.q_row | t.q_head) * g.esize);
+  const uint64_t low_o = (uint64_t)t.out | (uint64_t)((t.o_row | t.o_head) * g.esize);
+  if (!has_instance(g) || low % 16 || low_o % 4) {
+    const cs_status st = check_grid(b.n_rows, g.Hq, 1, kAnyThreads, "tree attention");
+    if (st || check_only) return st;
+    TraceScope tr("tree_attend_any", s);
+    const dim3 grid(b.n_rows, g.Hq);
+    if (g.dtype == CS_BF16) CS_LAUNCH(tr, tree_attend_any<uint16_t>, grid, dim3(kAnyThreads), 0, s, t);
+    else CS_LAUNCH(tr, tree_attend_any<float>, grid, dim3(kAnyThreads), 0, s, t);
+    return check_launch("tree attention launch");
+  }
+  if (check_only) return CS_OK;
+  const int nr = row_groups(g, b);
+  a.row_bits = nr == 1 ? 4 : nr == 2 ? 5 : 6;
+  a.tile_bits = g.dtype == CS_BF16 ? 5 : 4;
+  a.min_tiles = 2 * kWaves;
+  a.run_bits = kRunBits;
+  a.group = fast_div(g.G);
+  a.part = (float*)(((uintptr_t)ws + 255) & ~(uintptr_t)255);
+  a.part_ml = a.part + 2 * ((size_t)kRuns << a.row_bits) * g.D;
+  if (g.dtype == CS_BF16) {
+    switch (g.D) {
+      case 32: run_split<uint16_t, 32>(a, nr, s); break;
+      case 64: run_split<uint16_t, 64>(a, nr, s); break;
+      case 96: run_split<uint16_t, 96>(a, nr, s); break;
+      case 128: run_split<uint16_t, 128>(a, nr, s); break;
+      default: run_split<uint16_t, 256>(a, nr, s);
+    }
+  } else {
+    switch (g.D) {
+      case 16: run_split<float, 16>(a, nr, s); break;
+      case 32: run_split<float, 32>(a, nr, s); break;
+      case 64: run_split<float, 64>(a, nr, s); break;
+      default: run_split<float, 128>(a, nr, s);
+    }
+  }
   return check_launch("tree attention launch");
 }
 
