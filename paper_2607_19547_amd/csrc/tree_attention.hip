@@ -27,6 +27,13 @@ struct TreeArgs {
 __device__ __forceinline__ Request load_request(const TreeArgs& a, int b) {
   return request_of(a.row_start[b], a.row_start[b + 1], a.cached[b], a.n_rows, (int64_t)a.max_blocks * a.page.d);
 }
+// Arrays that no kernel of the call writes, at places that the whole wavefront
+// shares: through the scalar cache.
+typedef const __attribute__((address_space(4))) int32_t* scalar_ptr;
+__device__ __forceinline__ Request load_request_scalar(const TreeArgs& a, int b) {
+  const scalar_ptr rs = (scalar_ptr)(uint64_t)a.row_start, c = (scalar_ptr)(uint64_t)a.cached;
+  return request_of(rs[b], rs[b + 1], c[b], a.n_rows, (int64_t)a.max_blocks * a.page.d);
+}
 
 // Whether row i of a request sees its new row w (w >= 0).
 __device__ __forceinline__ bool sees(const TreeArgs& a, const Request& q, int i, int w) {
@@ -166,25 +173,22 @@ struct SplitArgs {
 };
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ int64_t uniform(int64_t x) {
-  return (int64_t)(((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32) | (uint32_t)uniform((int)x));
-}
-__device__ __forceinline__ Request uniform(Request q) {
-  q.r0 = uniform(q.r0);
-  q.n = uniform(q.n);
-  q.cached = uniform(q.cached);
-  q.len = uniform(q.len);
-  return q;
+__device__ __forceinline__ int64_t lane_value(int64_t x, int lane) {
+  return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32) |
+                   (uint32_t)__builtin_amdgcn_readlane((int)x, lane));
 }
 __device__ __forceinline__ void unit_sizes(const SplitArgs& a, const Request& q, int* nrt, int* ntile) {
   *nrt = (int)(((int64_t)q.n * a.t.G + (1 << a.row_bits) - 1) >> a.row_bits);
   *ntile = max((int)(((int64_t)q.len + (1 << a.tile_bits) - 1) >> a.tile_bits), 1);
 }
-// Unit of the key tile at `off` of a request, and the tile in it (a quotient
-// below 2^31 of numbers below 2^53).
+// x / d for 0 <= x < 2^53, d > 0 and a quotient below 2^31.
+__device__ __forceinline__ int quotient(int64_t x, int64_t d) {
+  const int u = (int)((double)x / (double)d);  // at most one too large, by rounding up
+  return u * d > x ? u - 1 : u;
+}
+// Unit of the key tile at `off` of a request, and the tile in it.
 __device__ __forceinline__ int unit_at(int64_t off, int ntile, int* tile) {
-  int u = (int)((double)off / (double)ntile);
-  if ((int64_t)u * ntile > off) --u;
+  const int u = quotient(off, ntile);
   *tile = (int)(off - (int64_t)u * ntile);
   return u;
 }
@@ -193,58 +197,45 @@ __device__ __forceinline__ int64_t run_length(const SplitArgs& a, int64_t total)
   return max((int64_t)a.min_tiles, (total + (1 << a.run_bits) - 1) >> a.run_bits);
 }
 
-struct RunShared {
-  int64_t red[kWaves];
-  int64_t off;
-  int b;
-};
 struct Run {
   int64_t begin, end, total, off;  // key tiles [begin, end) of `total`; begin is tile `off` of request b
   int b;
 };
-// Run w; false (for the whole workgroup) where there is none.
-__device__ __forceinline__ bool find_run(const SplitArgs& a, int w, RunShared& sh, Run* run) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int per = (a.t.B + kThreads - 1) / kThreads;
+// Run w; false where there is none.  Every wavefront finds it for itself: a
+// lane adds up a few consecutive requests, a prefix sum over the lanes gives
+// the lane whose requests hold the run's first tile, and that lane walks them.
+// Nothing waits for another wavefront.
+__device__ __forceinline__ bool find_run(const SplitArgs& a, int w, Run* run) {
+  const int lane = threadIdx.x & 63, per = (a.t.B + 63) >> 6;
   auto tiles = [&](int b) -> int64_t {
     int nrt, ntile;
     unit_sizes(a, load_request(a.t, b), &nrt, &ntile);
     return (int64_t)a.t.Hkv * nrt * ntile;
   };
+  const int b0 = min(lane * per, a.t.B), b1 = min(b0 + per, a.t.B);
   int64_t sum = 0;
-  for (int j = 0; j < per; ++j) {
-    const int b = tid * per + j;
-    if (b < a.t.B) sum += tiles(b);
-  }
-  const int64_t inc = wave_scan64(sum);
-  if (lane == 63) sh.red[wave] = inc;
-  __syncthreads();
-  int64_t before = 0, total = 0;
-#pragma unroll
-  for (int x = 0; x < kWaves; ++x) {
-    before += x < wave ? sh.red[x] : 0;
-    total += sh.red[x];
-  }
-  total = uniform(total);
+#pragma unroll 4
+  for (int b = b0; b < b1; ++b) sum += tiles(b);
+  const int64_t upto = wave_scan64(sum);
+  const int64_t total = lane_value(upto, 63);
   const int64_t len = run_length(a, total), begin = w * len;
   if (begin >= total) return false;
-  int64_t at = before + inc - sum;
-  if (begin >= at && begin < at + sum) {
-    int b = tid * per;
+  const int at = __builtin_ctzll(__ballot(upto > begin));  // the first lane that reaches past it
+  int64_t off = begin - lane_value(upto - sum, at);
+  int b = at * per;
+  if (per > 1)  // (the whole wavefront walks, off the scalar cache)
     for (;; ++b) {
-      const int64_t x = tiles(b);
-      if (begin < at + x) break;
-      at += x;
+      int nrt, ntile;
+      unit_sizes(a, load_request_scalar(a.t, b), &nrt, &ntile);
+      const int64_t x = (int64_t)a.t.Hkv * nrt * ntile;
+      if (off < x) break;
+      off -= x;
     }
-    sh.b = b;
-    sh.off = begin - at;
-  }
-  __syncthreads();
   run->begin = begin;
   run->end = min(begin + len, total);
   run->total = total;
-  run->off = uniform(sh.off);
-  run->b = uniform(sh.b);
+  run->off = off;
+  run->b = b;
   return true;
 }
 
@@ -303,13 +294,12 @@ __global__ __launch_bounds__(kThreads, NR * D * sizeof(E) <= 256 ? 2 : 1) void t
   constexpr int kPad = D + 4;
   static_assert(KS * 64 == kRowB && NO * 16 == D && VB % 4 == 0, "head dim");
 
-  __shared__ RunShared sh;
   __shared__ float s_o[kWaves * 16 * kPad];
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int ln = lane & 15, lg = lane >> 4;
   Run run;
-  if (!find_run(a, blockIdx.x, sh, &run)) return;
+  if (!find_run(a, blockIdx.x, &run)) return;
   const TreeArgs& t = a.t;
   int64_t left = run.end - run.begin, off = run.off;
   int b = run.b;
@@ -317,11 +307,9 @@ __global__ __launch_bounds__(kThreads, NR * D * sizeof(E) <= 256 ? 2 : 1) void t
   bool first_seg = true;
 
   while (left > 0) {
-    const Request q = uniform(load_request(t, b));
+    const Request q = load_request_scalar(t, b);
     int nrt, ntile;
     unit_sizes(a, q, &nrt, &ntile);
-    nrt = uniform(nrt);
-    ntile = uniform(ntile);
     if (off >= (int64_t)t.Hkv * nrt * ntile) {  // behind this request's units
       off = 0;
       ++b;
@@ -361,7 +349,6 @@ __global__ __launch_bounds__(kThreads, NR * D * sizeof(E) <= 256 ? 2 : 1) void t
     // the request's or the run's end.  The page numbers come through the scalar
     // cache, a tile ahead of the loads that need them, so that nothing waits
     // for the values in flight.
-    typedef const __attribute__((address_space(4))) int32_t* scalar_ptr;
     const scalar_ptr pages = (scalar_ptr)(uint64_t)table;
     int64_t at[SUB];
     int bytes[SUB], page[SUB];
@@ -684,83 +671,110 @@ __global__ __launch_bounds__(kThreads, NR * D * sizeof(E) <= 256 ? 2 : 1) void t
   }
 }
 
-// Merges the pieces of a unit that several workgroups worked on.  Workgroup
-// (w, y) looks at the border between runs w and w + 1: where it is the first
-// one inside a unit, it merges query vectors y, y + gridDim.y, ... of that unit.
-// 32 lanes hold one query vector's elements, the workgroup's groups of 32
-// take its pieces in turn.
+// Merges the pieces of a unit that several workgroups worked on, in key order.
+// Workgroup w has the border between runs w and w + 1.  The borders inside a
+// unit share its query vectors: the first takes vectors 0, n, 2n, ... of its n
+// borders, the next 1, n + 1, ...  32 lanes hold a vector's elements.  A unit
+// of many pieces (few requests, long caches) has as many borders, and all
+// eight groups of 32 lanes take pieces of one vector in turn; with few pieces
+// a group takes a vector for itself.  The pieces' weights are known before
+// their outputs are read, so those loads do not wait for each other.
 constexpr int kGroups = kThreads / 32;
+constexpr int kManyPieces = 16;
 template <typename E, int D>
 __global__ __launch_bounds__(kThreads) void tree_combine(const SplitArgs a) {
-  __shared__ RunShared sh;
-  __shared__ float s_o[kGroups][D], s_m[kGroups], s_l[kGroups];
-  constexpr int C = D / 32 > 0 ? D / 32 : 1;  // elements a lane holds
+  constexpr int C = (D + 31) / 32;  // elements a lane holds
+  __shared__ float s_o[kGroups][32 * C], s_m[kGroups], s_l[kGroups];
   const TreeArgs& t = a.t;
   const int w1 = blockIdx.x + 1;
   Run run;
-  if (!find_run(a, w1, sh, &run)) return;
-  const Request q = uniform(load_request(t, run.b));
+  if (!find_run(a, w1, &run)) return;
+  const Request q = load_request_scalar(t, run.b);
   int nrt, ntile, tile;
   unit_sizes(a, q, &nrt, &ntile);
   const int u = unit_at(run.off, ntile, &tile);
-  // only at the first border inside the unit
-  const int64_t len = run_length(a, run.total), unit0 = run.begin - tile, unit1 = unit0 + ntile, prev = run.begin - len;
-  if (tile == 0 || prev > unit0) return;
-  const int w0 = w1 - 1;
-  int w_last = w1;  // the run that holds the unit's last tile
-  while ((w_last + 1) * len < unit1) ++w_last;
-  const int pieces = w_last - w0 + 1;
+  if (tile == 0) return;  // the border lies between units
+  const int64_t len = run_length(a, run.total), unit0 = run.begin - tile, unit1 = unit0 + ntile;
+  const int w0 = quotient(unit0, len), w_last = quotient(unit1 - 1, len);  // the runs of its first and last tile
+  const int pieces = w_last - w0 + 1, borders = pieces - 1;
+  const int first = w0 * len < unit0 ? 1 : 0;  // the first piece ends its run, unless the run begins with the unit
   const int h = u / nrt, rt = u - h * nrt;
+  const int vectors = min(1 << a.row_bits, q.n * t.G - (rt << a.row_bits));
   const int grp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int r = blockIdx.y; r < 1 << a.row_bits && (rt << a.row_bits) + r < q.n * t.G; r += gridDim.y) {
+  const bool many = pieces > kManyPieces;
+  const int step = many ? kGroups : 1, x0 = many ? grp : 0;
+  // (many: every group has the same vectors, so the barriers below match)
+  for (int r = w1 - 1 - w0 + (many ? 0 : borders * grp); r < vectors; r += borders * (many ? 1 : kGroups)) {
     float M = -INFINITY, sum = 0.f, acc[C];
 #pragma unroll
     for (int e = 0; e < C; ++e) acc[e] = 0.f;
-    for (int x = grp; x < pieces; x += kGroups) {
-      // the first piece ends its run unless the run begins with the unit
-      const int64_t slot = 2 * (int64_t)(w0 + x) + (x == 0 && prev < unit0 ? 1 : 0);
-      const float* ml = a.part_ml + ((slot << a.row_bits) + r) * 2;
-      const float* pp = a.part + ((slot << a.row_bits) + r) * D + lane * C;
-      const float pm = ml[0], pl = ml[1];
-      float v[C];
-#pragma unroll
-      for (int e = 0; e < C; ++e) v[e] = lane * C + e < D ? pp[e] : 0.f;
-      if (pm == -INFINITY) {
-        if (M == -INFINITY) sum += pl;
-        continue;
+    for (int c = x0; c < pieces; c += 32 * step) {
+      const int mine = c + lane * step, cnt = min(32, (pieces - c + step - 1) / step);
+      float pm = -INFINITY, pl = 0.f;
+      const auto slot = [&](int x) { return 2 * (int64_t)(w0 + x) + (x == 0 ? first : 0); };
+      if (mine < pieces) {
+        const float2 ml = *(const float2*)(a.part_ml + ((slot(mine) << a.row_bits) + r) * 2);
+        pm = ml.x;
+        pl = ml.y;
       }
-      const float mn = fmaxf(M, pm);
-      const float wa = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - mn), wb = __builtin_amdgcn_exp2f(pm - mn);
-      sum = M == -INFINITY ? wb * pl : sum * wa + wb * pl;
+      float mx = pm;
 #pragma unroll
-      for (int e = 0; e < C; ++e) acc[e] = M == -INFINITY ? wb * v[e] : fmaf(acc[e], wa, wb * v[e]);
+      for (int o = 1; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+      const float mn = fmaxf(M, mx);
+      // a maximum of -inf has weight 0; where all are -inf the sums say whether
+      // a key was seen (NaN) or none (0)
+      const float w = pm == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(pm - mn);
+      float ps = pm == -INFINITY ? (mn == -INFINITY ? pl : 0.f) : w * pl;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) ps += __shfl_xor(ps, o);
+      const float back = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - mn);
+      sum = M == -INFINITY && mn != -INFINITY ? ps : fmaf(sum, mn == -INFINITY ? 1.f : back, ps);
+#pragma unroll
+      for (int e = 0; e < C; ++e) acc[e] *= back;
       M = mn;
+#pragma unroll 8
+      for (int y = 0; y < cnt; ++y) {
+        const float wy = __shfl(w, (threadIdx.x & 32) + y);
+        const float* pp = a.part + ((slot(c + y * step) << a.row_bits) + r) * D + lane * C;
+        float v[C];
+#pragma unroll
+        for (int e = 0; e < C; ++e) v[e] = D % 32 == 0 || lane * C + e < D ? pp[e] : 0.f;
+#pragma unroll
+        for (int e = 0; e < C; ++e) acc[e] += wy != 0.f ? wy * v[e] : 0.f;
+      }
     }
-    __syncthreads();
-    if (lane == 0) {
-      s_m[grp] = M;
-      s_l[grp] = sum;
+    if (many) {
+      __syncthreads();  // the previous vector has been read
+      if (lane == 0) {
+        s_m[grp] = M;
+        s_l[grp] = sum;
+      }
+#pragma unroll
+      for (int e = 0; e < C; ++e) s_o[grp][lane * C + e] = acc[e];
+      __syncthreads();
+      float Mt = -INFINITY;
+#pragma unroll
+      for (int x = 0; x < kGroups; ++x) Mt = fmaxf(Mt, s_m[x]);
+      sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < C; ++e) acc[e] = 0.f;
+#pragma unroll
+      for (int x = 0; x < kGroups; ++x) {
+        const float w = s_m[x] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[x] - Mt);
+        sum += s_m[x] == -INFINITY ? (Mt == -INFINITY ? s_l[x] : 0.f) : w * s_l[x];
+#pragma unroll
+        for (int e = 0; e < C; ++e) acc[e] += w != 0.f ? w * s_o[x][lane * C + e] : 0.f;
+      }
+      M = Mt;
+      if (grp) continue;
     }
+    const int qv = (rt << a.row_bits) + r, i = a.group.div(qv), head = h * t.G + qv - i * t.G;
+    const float inv = sum == 0.f && M == -INFINITY ? 0.f : 1.f / sum;
+    E* op = (E*)t.out + (q.r0 + i) * t.o_row + head * t.o_head + lane * C;
 #pragma unroll
     for (int e = 0; e < C; ++e)
-      if (lane * C + e < D) s_o[grp][lane * C + e] = acc[e];
-    __syncthreads();
-    float Mt = -INFINITY, lt = 0.f;
-#pragma unroll
-    for (int x = 0; x < kGroups; ++x) Mt = fmaxf(Mt, s_m[x]);
-#pragma unroll
-    for (int x = 0; x < kGroups; ++x)
-      lt += s_m[x] == -INFINITY ? (Mt == -INFINITY ? s_l[x] : 0.f) : __builtin_amdgcn_exp2f(s_m[x] - Mt) * s_l[x];
-    const int qv = (rt << a.row_bits) + r, i = a.group.div(qv), head = h * t.G + qv - i * t.G;
-    const float inv = lt == 0.f && Mt == -INFINITY ? 0.f : 1.f / lt;
-    for (int d = threadIdx.x; d < D; d += kThreads) {
-      float v = 0.f;
-#pragma unroll
-      for (int x = 0; x < kGroups; ++x)
-        if (s_m[x] != -INFINITY) v = fmaf(__builtin_amdgcn_exp2f(s_m[x] - Mt), s_o[x][d], v);
-      put_elem((E*)t.out + (q.r0 + i) * t.o_row + head * t.o_head + d, v * inv);
-    }
-    if (t.lse && threadIdx.x == 0) t.lse[(int64_t)(q.r0 + i) * t.Hq + head] = (Mt + __log2f(lt)) * kLn2;
+      if (D % 32 == 0 || lane * C + e < D) put_elem(op + e, acc[e] * inv);
+    if (t.lse && lane == 0) t.lse[(int64_t)(q.r0 + i) * t.Hq + head] = (M + __log2f(sum)) * kLn2;
   }
 }
 
@@ -795,7 +809,7 @@ static void run_split(const SplitArgs& a, hipStream_t s) {
     CS_LAUNCH(tr, (tree_attend<E, D, NR>), dim3(kRuns), dim3(kThreads), 0, s, a);
   }
   TraceScope tr("tree_combine", s);
-  CS_LAUNCH(tr, (tree_combine<E, D>), dim3(kRuns - 1, 16), dim3(kThreads), 0, s, a);
+  CS_LAUNCH(tr, (tree_combine<E, D>), dim3(kRuns - 1), dim3(kThreads), 0, s, a);
 }
 template <typename E, int D>
 static void run_split(const SplitArgs& a, int nr, hipStream_t s) {
