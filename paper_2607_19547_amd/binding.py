@@ -44,9 +44,10 @@ class Rows(ctypes.Structure):
 
     @classmethod
     def of(cls, t):
-        if t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] != 1):
+        stride = t.stride()
+        if len(stride) != 3 or stride[2] != 1:
             raise ValueError("rows are a tensor [n_rows, heads, D] with a contiguous last dimension")
-        return cls(t.data_ptr(), t.stride(0), t.stride(1))
+        return cls(t.data_ptr(), stride[0], stride[1])
 
 
 class _PagePool(ctypes.Structure):
@@ -163,11 +164,21 @@ def _ptr(t):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
+_raw_stream = None  # torch's lookup of a device's current stream as an address
+
+
 def _stream(stream):
+    """The address of the stream given, or of torch's current one (looked up without making a
+    Stream object where torch has that call: 0.3 us instead of 3)."""
     if stream is not None:
         return ctypes.c_void_p(stream)
+    global _raw_stream
     import torch
-    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    if _raw_stream is None:
+        torch.cuda.current_stream()  # (initialises the runtime, and says why where it cannot)
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda device: torch.cuda.current_stream(device).cuda_stream)
+    return ctypes.c_void_p(_raw_stream(torch.cuda.current_device()))
 
 
 def compose_rebase_k(geo, k_cache, chunk_offsets, local_coords=None, want_global=False, stream=None):
@@ -340,21 +351,31 @@ def selective_attend_scatter_rope_paged(geo, k_chunks, v_chunks, layer_begin, la
 
 
 # ---------------------------------------------------------------- batches over a pool of pages
+def _torch_dtype(dtype, _cache={}):
+    """torch's type of a geometry's dtype, or of a type's name."""
+    t = _cache.get(dtype)
+    if t is None:
+        import torch
+        _cache.update({CS_F32: torch.float32, CS_BF16: torch.bfloat16, "int32": torch.int32, "int64": torch.int64,
+                       "float32": torch.float32})
+        t = _cache[dtype]
+    return t
+
+
 def _array(t, name, dtype, shape, optional=False):
     """Device address of a dense tensor of the given type and shape (None in the shape: any size)."""
     if t is None:
         if optional:
             return None
         raise ValueError(f"{name} is required")
-    if str(t.dtype) != "torch." + dtype or not t.is_contiguous() or t.dim() != len(shape) or any(
-            want is not None and have != want for have, want in zip(t.shape, shape)):
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape}, got {t.dtype} {tuple(t.shape)}")
+    have = t.shape
+    if t.dtype is not _torch_dtype(dtype) or not t.is_contiguous() or (have != shape and (
+            len(have) != len(shape) or any(w is not None and w != h for h, w in zip(have, shape)))):
+        raise ValueError(f"{name} must be a contiguous {_torch_dtype(dtype)} tensor of shape {shape}, got {t.dtype} "
+                         f"{tuple(have)}")
     if not t.is_cuda:
         raise ValueError(f"{name} must be in device memory")
     return t.data_ptr()
-
-
-_TORCH_DTYPE = {CS_F32: "float32", CS_BF16: "bfloat16"}
 
 
 class PagePool:
@@ -364,8 +385,8 @@ class PagePool:
         shape = (None, geo.g.n_layers, geo.g.n_kv_heads, geo.g.n_tokens, geo.g.head_dim)
         self.tensors = (k_pages, v_pages)
         self.c = _PagePool()
-        self.c.k_pages = _array(k_pages, "k_pages", _TORCH_DTYPE[geo.g.dtype], shape)
-        self.c.v_pages = _array(v_pages, "v_pages", _TORCH_DTYPE[geo.g.dtype], (k_pages.shape[0],) + shape[1:])
+        self.c.k_pages = _array(k_pages, "k_pages", geo.g.dtype, shape)
+        self.c.v_pages = _array(v_pages, "v_pages", geo.g.dtype, (k_pages.shape[0],) + shape[1:])
         self.c.n_pages = k_pages.shape[0]
 
 
@@ -414,10 +435,11 @@ def _row_arg(t, name, geo, batch, heads):
     """A Rows, or a tensor that is checked and described."""
     if isinstance(t, Rows):
         return t
-    if str(t.dtype) != "torch." + _TORCH_DTYPE[geo.g.dtype] or not t.is_cuda or t.dim() != 3 or (
-            t.shape[0] < batch.c.n_rows or t.shape[1] != heads or t.shape[2] != geo.g.head_dim):
-        raise ValueError(f"{name} must be a {_TORCH_DTYPE[geo.g.dtype]} device tensor [{batch.c.n_rows}, {heads}, "
-                         f"{geo.g.head_dim}], got {t.dtype} {tuple(t.shape)}")
+    shape, d = t.shape, geo.g.head_dim
+    if t.dtype is not _torch_dtype(geo.g.dtype) or not t.is_cuda or len(shape) != 3 or (
+            shape[0] < batch.c.n_rows or shape[1] != heads or shape[2] != d):
+        raise ValueError(f"{name} must be a {_torch_dtype(geo.g.dtype)} device tensor [{batch.c.n_rows}, {heads}, "
+                         f"{d}], got {t.dtype} {tuple(shape)}")
     return Rows.of(t)
 
 
@@ -433,7 +455,7 @@ def qk_norm_rope_append(geo, pool, layer, batch, q, k, v, q_out, q_weight=None, 
                         stream=None):
     """Norm and rotation of the step's queries (to q_out) and keys; keys and values to their slots in `layer`."""
     hq, hkv = geo.g.n_q_heads, geo.g.n_kv_heads
-    w = [_array(x, "a weight", _TORCH_DTYPE[geo.g.dtype], (geo.g.head_dim,), optional=True)
+    w = [_array(x, "a weight", geo.g.dtype, (geo.g.head_dim,), optional=True)
          for x in (q_weight, k_weight)]
     _check(lib().qk_norm_rope_append(geo.ref, ctypes.byref(pool.c), int(layer), ctypes.byref(batch.c),
                                      ctypes.byref(_row_arg(q, "q", geo, batch, hq)),

@@ -5,42 +5,9 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "batch.h"
+#include "tree_attention.h"
 
 namespace cs {
-
-struct TreeArgs {
-  const void* q;
-  void* out;
-  float* lse;
-  int64_t q_row, q_head, o_row, o_head;  // strides in elements
-  const int32_t* cached;
-  const int32_t* row_start;
-  const int32_t* table;
-  const unsigned long long* mask;
-  PoolView pool;
-  FastDiv page;
-  int B, n_rows, max_blocks, words, layer, Hq, Hkv, G, D;
-  float scale;  // 1 / sqrt(D)
-};
-
-__device__ __forceinline__ Request load_request(const TreeArgs& a, int b) {
-  return request_of(a.row_start[b], a.row_start[b + 1], a.cached[b], a.n_rows, (int64_t)a.max_blocks * a.page.d);
-}
-// Arrays that no kernel of the call writes, at places that the whole wavefront
-// shares: through the scalar cache.
-typedef const __attribute__((address_space(4))) int32_t* scalar_ptr;
-__device__ __forceinline__ Request load_request_scalar(const TreeArgs& a, int b) {
-  const scalar_ptr rs = (scalar_ptr)(uint64_t)a.row_start, c = (scalar_ptr)(uint64_t)a.cached;
-  return request_of(rs[b], rs[b + 1], c[b], a.n_rows, (int64_t)a.max_blocks * a.page.d);
-}
-
-// Whether row i of a request sees its new row w (w >= 0).
-__device__ __forceinline__ bool sees(const TreeArgs& a, const Request& q, int i, int w) {
-  if (!a.mask) return w <= i;
-  if (w >> 6 >= a.words) return false;
-  return (a.mask[(int64_t)(q.r0 + i) * a.words + (w >> 6)] >> (w & 63)) & 1;
-}
 
 // ============================================================== any geometry
 // One workgroup per (row, query head), keys in blocks of 256: a thread scores
@@ -156,92 +123,10 @@ __global__ __launch_bounds__(kAnyThreads) void tree_attend_any(const TreeArgs a)
 // finds its run from the lengths alone (one load and a prefix sum).
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 // The running maximum may grow by 2^5 before the accumulators are rescaled:
 // probabilities stay far inside the range of both types.
 constexpr float kRescaleLog2 = 5.f;
 
-struct SplitArgs {
-  TreeArgs t;
-  float* part;      // [2 workgroups][row tile][D] unnormalised partial outputs
-  float* part_ml;   // [2 workgroups][row tile][2] their maximum (log2 units) and sum
-  int min_tiles;    // key tiles of a run at least
-  int row_bits;     // a row tile has 2^row_bits query vectors
-  int tile_bits;    // a key tile has 2^tile_bits keys
-  int run_bits;     // 2^run_bits runs at most
-  FastDiv group;    // division by G
-};
-
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ int64_t lane_value(int64_t x, int lane) {
-  return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32) |
-                   (uint32_t)__builtin_amdgcn_readlane((int)x, lane));
-}
-__device__ __forceinline__ void unit_sizes(const SplitArgs& a, const Request& q, int* nrt, int* ntile) {
-  *nrt = (int)(((int64_t)q.n * a.t.G + (1 << a.row_bits) - 1) >> a.row_bits);
-  *ntile = max((int)(((int64_t)q.len + (1 << a.tile_bits) - 1) >> a.tile_bits), 1);
-}
-// x / d for 0 <= x < 2^53, d > 0 and a quotient below 2^31.
-__device__ __forceinline__ int quotient(int64_t x, int64_t d) {
-  const int u = (int)((double)x / (double)d);  // at most one too large, by rounding up
-  return u * d > x ? u - 1 : u;
-}
-// Unit of the key tile at `off` of a request, and the tile in it.
-__device__ __forceinline__ int unit_at(int64_t off, int ntile, int* tile) {
-  const int u = quotient(off, ntile);
-  *tile = (int)(off - (int64_t)u * ntile);
-  return u;
-}
-// Key tiles of a run: the same for all, so that run w is [w x len, (w + 1) x len).
-__device__ __forceinline__ int64_t run_length(const SplitArgs& a, int64_t total) {
-  return max((int64_t)a.min_tiles, (total + (1 << a.run_bits) - 1) >> a.run_bits);
-}
-
-struct Run {
-  int64_t begin, end, total, off;  // key tiles [begin, end) of `total`; begin is tile `off` of request b
-  int b;
-};
-// Run w; false where there is none.  Every wavefront finds it for itself: a
-// lane adds up a few consecutive requests, a prefix sum over the lanes gives
-// the lane whose requests hold the run's first tile, and that lane walks them.
-// Nothing waits for another wavefront.
-__device__ __forceinline__ bool find_run(const SplitArgs& a, int w, Run* run) {
-  const int lane = threadIdx.x & 63, per = (a.t.B + 63) >> 6;
-  auto tiles = [&](int b) -> int64_t {
-    int nrt, ntile;
-    unit_sizes(a, load_request(a.t, b), &nrt, &ntile);
-    return (int64_t)a.t.Hkv * nrt * ntile;
-  };
-  const int b0 = min(lane * per, a.t.B), b1 = min(b0 + per, a.t.B);
-  int64_t sum = 0;
-#pragma unroll 4
-  for (int b = b0; b < b1; ++b) sum += tiles(b);
-  const int64_t upto = wave_scan64(sum);
-  const int64_t total = lane_value(upto, 63);
-  const int64_t len = run_length(a, total), begin = w * len;
-  if (begin >= total) return false;
-  const int at = __builtin_ctzll(__ballot(upto > begin));  // the first lane that reaches past it
-  int64_t off = begin - lane_value(upto - sum, at);
-  int b = at * per;
-  if (per > 1)  // (the whole wavefront walks, off the scalar cache)
-    for (;; ++b) {
-      int nrt, ntile;
-      unit_sizes(a, load_request_scalar(a.t, b), &nrt, &ntile);
-      const int64_t x = (int64_t)a.t.Hkv * nrt * ntile;
-      if (off < x) break;
-      off -= x;
-    }
-  run->begin = begin;
-  run->end = min(begin + len, total);
-  run->total = total;
-  run->off = off;
-  run->b = b;
-  return true;
-}
-
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const char* base, int bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00020000);
-}
 template <int BYTES>
 struct Words {
   uint32_t w[BYTES / 4];
@@ -796,10 +681,17 @@ static int row_groups(const Geo& g, const cs_batch& b) {
   return qv <= 16 ? 1 : qv <= 32 ? 2 : 4;
 }
 
+// Whether the kernel for many rows takes the batch (where its pointers are aligned).
+static bool wide(const Geo& g, const cs_batch& b) {
+  const int64_t rows = b.max_rows > 0 ? b.max_rows : b.n_rows;
+  return g.dtype == CS_BF16 && g.D == 128 && g.T % 16 == 0 && rows * g.G > 64;
+}
+
 size_t tree_attend_workspace(const Geo& g, const cs_batch& b) {
   if (!has_instance(g)) return 0;
   const size_t rows = 16 * (size_t)row_groups(g, b);
-  return 2 * (size_t)kRuns * rows * (g.D + 2) * sizeof(float) + 512;
+  const size_t few = 2 * (size_t)kRuns * rows * (g.D + 2) * sizeof(float) + 512;
+  return wide(g, b) ? std::max(few, tree_wide_workspace()) : few;
 }
 
 template <typename E, int D, int NR>
@@ -858,12 +750,16 @@ cs_status launch_tree_attend(const Geo& g, const cs_page_pool& pool, int layer, 
     return check_launch("tree attention launch");
   }
   if (check_only) return CS_OK;
+  a.group = fast_div(g.G);
+  if (wide(g, b) && low_o % 8 == 0) {
+    launch_tree_wide(a, ws, s);
+    return check_launch("tree attention launch");
+  }
   const int nr = row_groups(g, b);
   a.row_bits = nr == 1 ? 4 : nr == 2 ? 5 : 6;
   a.tile_bits = g.dtype == CS_BF16 ? 5 : 4;
   a.min_tiles = 2 * kWaves;
   a.run_bits = kRunBits;
-  a.group = fast_div(g.G);
   a.part = (float*)(((uintptr_t)ws + 255) & ~(uintptr_t)255);
   a.part_ml = a.part + 2 * ((size_t)kRuns << a.row_bits) * g.D;
   if (g.dtype == CS_BF16) {

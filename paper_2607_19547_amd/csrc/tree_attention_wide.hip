@@ -1,0 +1,539 @@
+// Attention of a batch's rows over their requests' pages for requests of many
+// rows: trees of drafted tokens and questions (bf16, head_dim 128).
+//
+// With many query vectors the products bound the work, not the reading of the
+// keys, so a K/V tile is staged in LDS once for 256 query vectors of a KV head:
+// eight wavefronts of 32, two per SIMD.  Per 64-key tile a wavefront computes
+//   S^T = K Q^T       (v_mfma_f32_32x32x16_bf16, K from LDS, Q in registers)
+//   O^T += V^T P^T    (V^T by transposing reads of LDS, P^T from the scores' registers)
+// with the softmax on the 32 scores of one query that a lane holds, in one
+// block with the next tile's S^T, so that exponentials and products overlap.
+// Tiles come by buffer-to-LDS loads into a ring of four, three ahead: one
+// wavefront brings 8 keys, whose page it looks up through the scalar cache
+// (pages are multiples of 16 tokens); rows behind the request's end, and rows
+// of no page of the pool, read as zeros.
+//
+// The work is cut as in the kernel for few rows (equal runs of key tiles, one
+// run for each of 256 workgroups, one workgroup per CU); pieces of a unit
+// leave float32 partials in the accumulators' own layout.
+#include <math.h>
+
+#include <type_traits>
+
+#include "tree_attention.h"
+
+namespace cs {
+
+constexpr int kKT = 64;                  // keys per tile
+constexpr int kWideWaves = 8;
+constexpr int kWideThreads = 64 * kWideWaves;
+constexpr int kRow = 256;                // bytes of a K/V row
+constexpr int kHiLds = 65536;            // LDS bytes below the K ring (the V ring)
+constexpr float kRescaleLog2 = 5.f;      // growth of the running maximum before the accumulators are rescaled
+constexpr int kWideRuns = 1 << kWideRunBits;
+constexpr int kPartFloats = 256 * 128;   // a partial's outputs
+
+typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+typedef __attribute__((address_space(3))) void lds_void;
+
+// Lanes l and l ^ 32 hold the same query.
+__device__ __forceinline__ float pair_max(float x) {
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float pair_sum(float x) {
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+__global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs a0) {
+  // LDS rows are 256 bytes, a key each, their 16-byte chunks permuted so that
+  // the operand reads are free of bank conflicts (K: chunk c of row r at c ^
+  // (r & 15); V: at c ^ 4 (r & 3)).  The V ring takes the low 64 KB, where the
+  // DS instructions' 16-bit offsets reach; variables are laid out by name.
+  __shared__ __attribute__((aligned(1024))) char lo_v0[kKT * kRow], lo_v1[kKT * kRow], lo_v2[kKT * kRow], lo_v3[kKT * kRow];
+  __shared__ __attribute__((aligned(1024))) char up_k0[kKT * kRow], up_k1[kKT * kRow], up_k2[kKT * kRow], up_k3[kKT * kRow];
+  auto kbuf = [&](auto B) -> char* {
+    if constexpr (decltype(B)::value == 0) return up_k0;
+    else if constexpr (decltype(B)::value == 1) return up_k1;
+    else if constexpr (decltype(B)::value == 2) return up_k2;
+    else return up_k3;
+  };
+  auto vbuf = [&](auto B) -> char* {
+    if constexpr (decltype(B)::value == 0) return lo_v0;
+    else if constexpr (decltype(B)::value == 1) return lo_v1;
+    else if constexpr (decltype(B)::value == 2) return lo_v2;
+    else return lo_v3;
+  };
+  using I0 = std::integral_constant<int, 0>;
+  using I1 = std::integral_constant<int, 1>;
+  using I2 = std::integral_constant<int, 2>;
+  using I3 = std::integral_constant<int, 3>;
+
+  // The arguments are read again where they are used, so that the tile loop
+  // keeps none of them in registers.
+  typedef const __attribute__((address_space(4))) SplitArgs* ArgPtr;
+  const ArgPtr argp = (ArgPtr)__builtin_amdgcn_kernarg_segment_ptr();
+  auto args = [&]() -> SplitArgs {
+    ArgPtr p = argp;
+    asm volatile("" : "+s"(p));
+    return *(const SplitArgs*)p;
+  };
+  const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, ql = lane & 31, hi = lane >> 5;
+
+  Run run;
+  if (!find_run(a0, blockIdx.x, &run)) return;
+  int64_t left = run.end - run.begin, off = run.off;
+  int b = run.b;
+  bool first_seg = true;
+
+  int koff[8];  // K operand: row ql, chunk 2s + hi (row 32 + ql has the same swizzle)
+#pragma unroll
+  for (int s = 0; s < 8; ++s) {
+    koff[s] = ql * kRow + 16 * ((2 * s + hi) ^ (ql & 15));
+    // opaque to constant folding, so that each read keeps this register as its
+    // base and puts (slot - kHiLds) in the instruction's offset field
+    asm("v_add_u32 %0, 0x10000, %1" : "=v"(koff[s]) : "v"(koff[s]));
+  }
+  const int vl = lane & 15, dh = (lane >> 4) & 1;
+  int voff[4];  // V transposing reads: rows 4hi + vl/4 (+16ks, +8), dims 32d + 16dh + 4(vl%4)
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+    voff[d] = (4 * hi + (vl >> 2)) * kRow + 16 * ((4 * d + 2 * dh + ((vl & 3) >> 1)) ^ ((vl >> 2) << 2)) + 8 * (vl & 1);
+  int soff_k[2], soff_v[2];  // this lane's chunk within the wavefront's 8 keys, per load
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int r = 4 * j + (lane >> 4), tr = 8 * wave + r, p = lane & 15;
+    soff_k[j] = r * kRow + 16 * (p ^ (tr & 15));
+    soff_v[j] = r * kRow + 16 * (p ^ ((tr & 3) << 2));
+  }
+  const float sc = a0.t.scale * kLog2e;
+
+  while (left > 0) {
+    Request q;
+    int u, t0, nrt, ntile;
+    {
+      const SplitArgs A = args();
+      q = load_request_scalar(A.t, b);
+      unit_sizes(A, q, &nrt, &ntile);
+      if (off >= (int64_t)A.t.Hkv * nrt * ntile) {  // behind this request's units
+        off = 0;
+        ++b;
+        continue;
+      }
+    }
+    u = uniform(unit_at(off, ntile, &t0));
+    t0 = uniform(t0);
+    const int seg = (int)min(left, (int64_t)(ntile - t0));
+    const int h = uniform(u / nrt), rt = u - h * nrt;
+    int n_kt, key_begin, g_row, w_seen, bad;  // g_row: the lane's row; w_seen: keys behind it are seen by no row of the wavefront
+    bf16x8 qb[8];
+    {
+      const SplitArgs A = args();
+      const int vectors = q.n * A.t.G;
+      // rows see no key behind their own without a mask, so later tiles are left out
+      const int i_last = A.group.div(min((rt + 1) * 256, vectors) - 1);
+      const int key_end = A.t.mask ? q.len : min(q.len, q.cached + i_last + 1);
+      key_begin = t0 * kKT;
+      n_kt = max(min(t0 + seg, (key_end + kKT - 1) / kKT) - t0, 0);
+      const int v0 = rt * 256 + 32 * wave;
+      const int qv = min(v0 + ql, vectors - 1);
+      g_row = A.group.div(qv);
+      w_seen = v0 >= vectors ? -1 : A.t.mask ? q.len : q.cached + uniform(A.group.div(min(v0 + 31, vectors - 1)));
+      const uint16_t* qp = (const uint16_t*)A.t.q + (int64_t)(q.r0 + g_row) * A.t.q_row +
+                           (h * A.t.G + qv - g_row * A.t.G) * A.t.q_head + 8 * hi;
+#pragma unroll
+      for (int s = 0; s < 8; ++s) qb[s] = *(const bf16x8*)(qp + 16 * s);
+      // pages of this piece that are none of the pool
+      bad = 0;
+      if (n_kt > 0) {
+        const int p0 = A.t.page.div(key_begin), p1 = A.t.page.div(min(key_begin + n_kt * kKT, q.len) - 1);
+        const int32_t* tb = A.t.table + (int64_t)b * A.t.max_blocks;
+        for (int x = p0 + tid; x <= p1; x += kWideThreads) bad |= tb[x] < 0 || tb[x] >= A.t.pool.n_pages;
+      }
+    }
+    bad = __syncthreads_or(bad);  // (the ring is free as well: every wavefront has left the previous piece)
+
+    // this wavefront's 8 keys of tile i: their page, and the loads into a ring slot
+    int page_next = 0;
+    auto find_page = [&](int i) {
+      const SplitArgs A = args();
+      const scalar_ptr tb = (scalar_ptr)(uint64_t)(A.t.table + (int64_t)b * A.t.max_blocks);
+      if (q.len > 0) page_next = tb[A.t.page.div(min(key_begin + i * kKT + 8 * wave, q.len - 1))];
+    };
+    auto fetch = [&](int i, char* Kd, char* Vd) {
+      const SplitArgs A = args();
+      const int key = key_begin + i * kKT + 8 * wave;
+      const bool ok = i < n_kt && key < q.len && page_next >= 0 && page_next < A.t.pool.n_pages;
+      int64_t at = 0;
+      int bytes = 0;
+      if (ok) {
+        at = page_next * A.t.pool.page_bytes +
+             (((int64_t)A.t.layer * A.t.Hkv + h) * A.t.page.d + key - A.t.page.div(key) * A.t.page.d) * kRow;
+        bytes = min(q.len - key, 8) * kRow;
+      }
+      const auto rk = rows_rsrc(A.t.pool.k + at, bytes), rv = rows_rsrc(A.t.pool.v + at, bytes);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int r0 = 8 * wave + 4 * j;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void*)(Kd + r0 * kRow), 16, soff_k[j], 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void*)(Vd + r0 * kRow), 16, soff_v[j], 0, 0, 0);
+      }
+      find_page(i + 1);
+    };
+    find_page(0);
+    fetch(0, up_k0, lo_v0);
+    fetch(1, up_k1, lo_v1);
+    fetch(2, up_k2, lo_v2);
+
+    f32x16 o[4];
+#pragma unroll
+    for (int d = 0; d < 4; ++d) o[d] = f32x16{};
+    float m_use = -INFINITY, l_run = 0.f;
+    bool seen = false;
+
+    auto qk = [&](auto B, f32x16& s0, f32x16& s1) {
+      const char* K = kbuf(B);
+      s0 = f32x16{};
+      s1 = f32x16{};
+#pragma unroll
+      for (int s = 0; s < 8; ++s) {
+        const bf16x8 k0 = *(const bf16x8*)(K - kHiLds + koff[s]);
+        const bf16x8 k1 = *(const bf16x8*)(K - kHiLds + 32 * kRow + koff[s]);
+        s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k0, qb[s], s0, 0, 0, 0);
+        s1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k1, qb[s], s1, 0, 0, 0);
+      }
+    };
+    // V operand of 16 keys ks and 32 dims d
+    auto v_operand = [&](const char* V, int ks, int d) {
+      const char* vp = V + ks * 16 * kRow + voff[d];
+      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(vp));
+      const bf16x4 up = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(vp + 8 * kRow));
+      return __builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+
+    // Tiles with the step's own rows, the request's end or keys in no page of
+    // the pool: the keys that the lane's row does not see get -inf.
+    // Accumulator register r of block y holds key kt + 32 y + 8 (r / 4) + 4 hi + r % 4.
+    auto visible = [&](int kt) -> uint64_t {  // bit 32 y + 8 (r / 4) + r % 4 belongs to register r of block y
+      const SplitArgs A = args();
+      uint64_t vis;
+      {
+        const int w0 = kt - q.cached, w = max(w0, 0);
+        uint64_t bits = 0;
+        if (A.t.mask) {
+          const unsigned long long* mk = A.t.mask + (int64_t)(q.r0 + g_row) * A.t.words;
+          const int j = w >> 6, sft = w & 63;
+          if (w0 > -kKT && j < A.t.words) bits = mk[j] >> sft;
+          if (w0 > -kKT && sft && j + 1 < A.t.words) bits |= mk[j + 1] << (64 - sft);
+        } else {
+          const int n = g_row - w + 1;
+          bits = n >= 64 ? ~0ull : n > 0 ? (1ull << n) - 1 : 0ull;
+        }
+        vis = w0 <= -64 ? ~0ull : w0 < 0 ? bits << -w0 | ((1ull << -w0) - 1) : bits;
+        const int n = q.len - kt;
+        vis &= n >= 64 ? ~0ull : (1ull << n) - 1;
+        if (bad) {
+          const scalar_ptr tb = (scalar_ptr)(uint64_t)(A.t.table + (int64_t)b * A.t.max_blocks);
+          for (int y = 0; y < 4; ++y) {
+            const int pg = tb[A.t.page.div(min(kt + 16 * y, q.len - 1))];
+            if (pg < 0 || pg >= A.t.pool.n_pages) vis &= ~(0xffffull << (16 * y));
+          }
+        }
+      }
+      seen = seen || vis != 0;
+      return vis >> (4 * hi);
+    };
+    auto mask = [&](int kt, f32x16& s0, f32x16& s1) {
+      const uint64_t mine = visible(kt);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int bit = 8 * (r >> 2) + (r & 3);
+        if (!((uint32_t)mine >> bit & 1)) s0[r] = -INFINITY;
+        if (!((uint32_t)(mine >> 32) >> bit & 1)) s1[r] = -INFINITY;
+      }
+    };
+    // Values that are not finite must not reach rows that do not see them
+    // (0 x inf).  Where the tile has one (every wavefront finds the same), the
+    // products count, for each output element, the values of +inf (or NaN) and
+    // of -inf (or NaN) that its row sees; those give it the infinity, both of
+    // them NaN.  Then the values become zero in LDS.  (After the accumulators
+    // are rescaled for the tile: their first factor is 0.)
+    auto not_finite = [&](auto C, int kt) {
+      char* V = vbuf(C);
+      uint32_t odd = 0;
+      for (int x = lane; x < kKT * kRow / 16; x += 64) {
+        const u32x4 v = *(const u32x4*)(V + 16 * x);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) odd |= (v[y] & 0x7f807f80u) + 0x00800080u;
+      }
+      if (__ballot(odd & 0x80008000u)) {
+        const uint64_t mine = visible(kt);
+#pragma unroll 1
+        for (int sign = 0; sign < 2; ++sign) {
+          auto flag = [&](uint32_t v) -> uint32_t {  // 1.0 in bf16 where the element counts
+            const bool nan = (v & 0x7f80u) == 0x7f80u && (v & 0x7fu);
+            return nan || (v & 0xffffu) == (sign ? 0xff80u : 0x7f80u) ? 0x3f80u : 0u;
+          };
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            f32x16 c = f32x16{};
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) {
+              u32x4 va = __builtin_bit_cast(u32x4, v_operand(V, ks, d)), pb;
+#pragma unroll
+              for (int y = 0; y < 4; ++y) va[y] = flag(va[y]) | flag(va[y] >> 16) << 16;
+              // the operand's elements x are registers 8 (ks & 1) + x of block ks / 2
+              const uint32_t bits = (uint32_t)(mine >> (32 * (ks >> 1) + 16 * (ks & 1)));
+#pragma unroll
+              for (int y = 0; y < 4; ++y) {
+                const int b0 = 8 * (y >> 1) + 2 * (y & 1);
+                pb[y] = (bits >> b0 & 1 ? 0x3f80u : 0u) | (bits >> (b0 + 1) & 1 ? 0x3f800000u : 0u);
+              }
+              c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, va), __builtin_bit_cast(bf16x8, pb), c, 0, 0, 0);
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              if (c[r] > 0.f) o[d][r] += sign ? -INFINITY : INFINITY;
+          }
+        }
+        __syncthreads();  // every wavefront has read the tile
+        for (int x = tid; x < kKT * kRow / 4; x += kWideThreads) {
+          uint32_t v = *(const uint32_t*)(V + 4 * x);
+          if ((v & 0x7f80u) == 0x7f80u) v &= 0xffff0000u;
+          if ((v & 0x7f800000u) == 0x7f800000u) v &= 0xffffu;
+          *(uint32_t*)(V + 4 * x) = v;
+        }
+        __syncthreads();
+      }
+    };
+
+    // Running maximum of the tile; rescales the accumulators when it grew by more than 2^5.
+    auto tile_max = [&](f32x16& s0, f32x16& s1) {
+      float t8[8];
+#pragma unroll
+      for (int r = 0; r < 8; ++r) t8[r] = fmaxf(fmaxf(s0[r], s0[r + 8]), s1[r]);
+      float t4[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) t4[r] = fmaxf(fmaxf(t8[2 * r], t8[2 * r + 1]), s1[r + 8]);
+      const float t2a = fmaxf(fmaxf(t4[0], t4[1]), s1[12]), t2b = fmaxf(fmaxf(t4[2], t4[3]), s1[13]);
+      const float mx = fmaxf(fmaxf(fmaxf(t2a, t2b), s1[14]), s1[15]);
+      const float mt = pair_max(mx) * sc;
+      const bool need = mt > m_use + kRescaleLog2;
+      if (__ballot(need)) {
+        const float m_new = need ? mt : m_use;
+        const float alpha = need ? __builtin_amdgcn_exp2f(m_use - m_new) : 1.f;
+        l_run *= alpha;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) o[d] *= alpha;
+        m_use = m_new;
+      }
+    };
+    auto qk_head = [&](auto N, f32x16& n0, f32x16& n1) {
+      const char* K = kbuf(N);
+      n0 = f32x16{};
+      n1 = f32x16{};
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const bf16x8 k0 = *(const bf16x8*)(K - kHiLds + koff[s]);
+        const bf16x8 k1 = *(const bf16x8*)(K - kHiLds + 32 * kRow + koff[s]);
+        n0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k0, qb[s], n0, 0, 0, 0);
+        n1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k1, qb[s], n1, 0, 0, 0);
+      }
+    };
+    // Probabilities of the current tile, O^T += V^T P^T, and k-steps 2..7 of
+    // the next tile's S^T in one straight-line block.
+    auto exp_pv_qk = [&](auto C, auto N, f32x16& s0, f32x16& s1, f32x16& n0, f32x16& n1) {
+      const char* V = vbuf(C);
+      const char* K = kbuf(N);
+      __builtin_amdgcn_iglp_opt(3);
+      const float nm = m_use == -INFINITY ? 0.f : -m_use;
+      bf16x8 pb[4];
+      float ls[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) {
+        const f32x16& sv = ks < 2 ? s0 : s1;
+        const int base = 8 * (ks & 1);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(sv[base + x], sc, nm));
+          ls[ks] += p;  // (the sum of the unrounded probabilities)
+          pb[ks][x] = (__bf16)p;
+        }
+        if (ks < 3) {
+#pragma unroll
+          for (int s = 2 * ks + 2; s < 2 * ks + 4; ++s) {
+            const bf16x8 k0 = *(const bf16x8*)(K - kHiLds + koff[s]);
+            const bf16x8 k1 = *(const bf16x8*)(K - kHiLds + 32 * kRow + koff[s]);
+            n0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k0, qb[s], n0, 0, 0, 0);
+            n1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k1, qb[s], n1, 0, 0, 0);
+          }
+        }
+#pragma unroll
+        for (int d = 0; d < 4; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(V, ks, d), pb[ks], o[d], 0, 0, 0);
+      }
+      l_run += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+    };
+
+    // Tile i is in ring slot C, tile i + 1 in N; tile i + 3 goes to S (read last
+    // in step i - 1).  Each wavefront waits for its part of tile i + 2 (all but
+    // its four newest loads) before the barrier.
+    const int t_clear = bad ? 0 : min(q.cached, q.len) / kKT - t0;  // tiles before it need no mask
+    auto step = [&](auto C, auto N, auto S, int i, f32x16& c0, f32x16& c1, f32x16& n0, f32x16& n1) {
+      const int kt = key_begin + i * kKT;
+      fetch(i + 3, kbuf(S), vbuf(S));
+      if (i >= t_clear) mask(kt, c0, c1);
+      else seen = true;
+      if (kt <= w_seen) {
+        qk_head(N, n0, n1);
+        tile_max(c0, c1);
+      }
+      if (i >= t_clear) not_finite(C, kt);  // (has barriers: every wavefront)
+      if (kt <= w_seen) exp_pv_qk(C, N, c0, c1, n0, n1);
+      asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+    };
+    f32x16 sa0, sa1, sb0, sb1;
+    asm volatile("s_waitcnt vmcnt(4)" ::: "memory");  // tiles 0 and 1 and the queries have landed
+    __builtin_amdgcn_s_barrier();
+    qk(I0{}, sa0, sa1);
+    for (int i = 0; i < n_kt; i += 4) {
+      step(I0{}, I1{}, I3{}, i, sa0, sa1, sb0, sb1);
+      if (i + 1 >= n_kt) break;
+      step(I1{}, I2{}, I0{}, i + 1, sb0, sb1, sa0, sa1);
+      if (i + 2 >= n_kt) break;
+      step(I2{}, I3{}, I1{}, i + 2, sa0, sa1, sb0, sb1);
+      if (i + 3 >= n_kt) break;
+      step(I3{}, I0{}, I2{}, i + 3, sb0, sb1, sa0, sa1);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+
+    // Results: accumulator register r of block d holds dim 32d + 8(r/4) + 4hi + r%4.
+    const SplitArgs A = args();
+    const int vectors = q.n * A.t.G, qv = rt * 256 + 32 * wave + ql;
+    float lt = pair_sum(l_run);
+    if (seen && m_use == -INFINITY) lt = __uint_as_float(0x7fc00000u);  // only scores of -inf were seen
+    if (seg == ntile) {
+      if (qv < vectors) {
+        const int head = h * A.t.G + qv - g_row * A.t.G;
+        const float inv = m_use == -INFINITY && lt == 0.f ? 0.f : 1.f / lt;
+        uint16_t* op = (uint16_t*)A.t.out + (int64_t)(q.r0 + g_row) * A.t.o_row + head * A.t.o_head + 4 * hi;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            u32x2 w;
+            w[0] = pack_bf16x2(o[d][4 * r] * inv, o[d][4 * r + 1] * inv);
+            w[1] = pack_bf16x2(o[d][4 * r + 2] * inv, o[d][4 * r + 3] * inv);
+            *(u32x2*)(op + 32 * d + 8 * r) = w;
+          }
+        if (A.t.lse && hi == 0) A.t.lse[(int64_t)(q.r0 + g_row) * A.t.Hq + head] = (m_use + __log2f(lt)) * kLn2;
+      }
+    } else {
+      const int64_t slot = 2 * (int64_t)blockIdx.x + (first_seg ? 0 : 1);
+      if (hi == 0) *(float2*)(A.part_ml + (slot * 256 + 32 * wave + ql) * 2) = make_float2(m_use, lt);
+      float* pp = A.part + slot * kPartFloats + wave * (16 * 256) + lane * 4;
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          *(f32x4*)(pp + (4 * d + r) * 256) = f32x4{o[d][4 * r], o[d][4 * r + 1], o[d][4 * r + 2], o[d][4 * r + 3]};
+    }
+    first_seg = false;
+    left -= seg;
+    off += seg;
+    __syncthreads();  // the ring is free
+  }
+}
+
+// Merges the pieces of a unit, in key order.  A wavefront takes the same 16
+// bytes of 32 query vectors' halves (one store of a piece's wavefront: 1 KB in
+// a row) through all pieces; the unit's 128 such strips are shared by the
+// workgroups of the borders inside it.
+constexpr int kStripThreads = 256;
+__global__ __launch_bounds__(kStripThreads) void tree_combine_wide(const SplitArgs a) {
+  const TreeArgs& t = a.t;
+  const int w1 = blockIdx.x + 1;
+  Run run;
+  if (!find_run(a, w1, &run)) return;
+  const Request q = load_request_scalar(t, run.b);
+  int nrt, ntile, tile;
+  unit_sizes(a, q, &nrt, &ntile);
+  const int u = unit_at(run.off, ntile, &tile);
+  if (tile == 0) return;  // the border lies between units
+  const int64_t len = run_length(a, run.total), unit0 = run.begin - tile;
+  const int w0 = quotient(unit0, len), w_last = quotient(unit0 + ntile - 1, len);
+  const int pieces = w_last - w0 + 1, borders = pieces - 1;
+  const int first = w0 * len < unit0 ? 1 : 0;
+  const int h = u / nrt, rt = u - h * nrt, vectors = q.n * t.G;
+  const int lane = threadIdx.x & 63, ql = lane & 31, hi = lane >> 5;
+  for (int strip = (w1 - 1 - w0) * 4 + uniform(threadIdx.x >> 6); strip < 128; strip += borders * 4) {
+    const int wave = strip >> 4, c = strip & 15, qv = rt * 256 + 32 * wave + ql;
+    if (rt * 256 + 32 * wave >= vectors) break;  // (strips ascend)
+    float M = -INFINITY, sum = 0.f;
+    f32x4 acc = f32x4{};
+    constexpr int U = 8;
+    for (int x = 0; x < pieces; x += U) {
+      float2 ml[U];
+      f32x4 v[U];
+#pragma unroll
+      for (int y = 0; y < U; ++y) {
+        const int p = min(x + y, pieces - 1);
+        const int64_t slot = 2 * (int64_t)(w0 + p) + (p == 0 ? first : 0);
+        ml[y] = *(const float2*)(a.part_ml + (slot * 256 + 32 * wave + ql) * 2);
+        v[y] = *(const f32x4*)(a.part + slot * kPartFloats + strip * 256 + lane * 4);
+      }
+      float mn = M;
+#pragma unroll
+      for (int y = 0; y < U; ++y) mn = fmaxf(mn, x + y < pieces ? ml[y].x : -INFINITY);
+      if (M != -INFINITY) {
+        const float back = __builtin_amdgcn_exp2f(M - mn);
+        sum *= back;
+        acc *= back;
+      } else if (mn != -INFINITY) {
+        sum = 0.f;  // (pieces of scores of -inf alone do not count beside others)
+      }
+#pragma unroll
+      for (int y = 0; y < U; ++y) {
+        if (x + y >= pieces) continue;
+        if (ml[y].x == -INFINITY) {
+          if (mn == -INFINITY) sum += ml[y].y;
+          continue;
+        }
+        const float w = __builtin_amdgcn_exp2f(ml[y].x - mn);
+        sum = fmaf(w, ml[y].y, sum);
+        if (w != 0.f)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[e] = fmaf(w, v[y][e], acc[e]);
+      }
+      M = mn;
+    }
+    if (qv >= vectors) continue;
+    const int i = a.group.div(qv), head = h * t.G + qv - i * t.G;
+    const float inv = M == -INFINITY && sum == 0.f ? 0.f : 1.f / sum;
+    u32x2 w;
+    w[0] = pack_bf16x2(acc[0] * inv, acc[1] * inv);
+    w[1] = pack_bf16x2(acc[2] * inv, acc[3] * inv);
+    *(u32x2*)((uint16_t*)t.out + (int64_t)(q.r0 + i) * t.o_row + head * t.o_head + 32 * (c >> 2) + 8 * (c & 3) + 4 * hi) = w;
+    if (t.lse && c == 0 && hi == 0) t.lse[(int64_t)(q.r0 + i) * t.Hq + head] = (M + __log2f(sum)) * kLn2;
+  }
+}
+
+size_t tree_wide_workspace() { return 2 * (size_t)kWideRuns * (kPartFloats + 2 * 256) * sizeof(float) + 512; }
+
+void launch_tree_wide(SplitArgs a, void* ws, hipStream_t s) {
+  a.row_bits = kWideRowBits;
+  a.tile_bits = kWideTileBits;
+  a.run_bits = kWideRunBits;
+  a.min_tiles = 4;
+  a.part = (float*)(((uintptr_t)ws + 255) & ~(uintptr_t)255);
+  a.part_ml = a.part + 2 * (size_t)kWideRuns * kPartFloats;
+  {
+    TraceScope tr("tree_attend_wide", s);
+    CS_LAUNCH(tr, tree_attend_wide, dim3(kWideRuns), dim3(kWideThreads), 0, s, a);
+  }
+  TraceScope tr("tree_combine_wide", s);
+  CS_LAUNCH(tr, tree_combine_wide, dim3(kWideRuns - 1), dim3(kStripThreads), 0, s, a);
+}
+
+}  // namespace cs
