@@ -132,6 +132,44 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const char* base, in
   return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00020000);
 }
 
+// Pieces of one query vector's softmax, merged a round at a time: maxima (log2
+// units) and sums, and C elements of the outputs.  A piece whose maximum is
+// -inf saw no key (sum 0) or scores of -inf alone (sum NaN): it counts only
+// where all are like that.
+template <int C>
+struct Merge {
+  float m = -INFINITY, sum = 0.f, acc[C] = {};
+  template <int U>
+  __device__ __forceinline__ void add(const float2 (&ml)[U], const float (&v)[U][C]) {
+    float mn = m;
+#pragma unroll
+    for (int y = 0; y < U; ++y) mn = fmaxf(mn, ml[y].x);
+    if (m != -INFINITY) {
+      const float back = __builtin_amdgcn_exp2f(m - mn);
+      sum *= back;
+#pragma unroll
+      for (int e = 0; e < C; ++e) acc[e] *= back;
+    } else if (mn != -INFINITY) {
+      sum = 0.f;
+    }
+#pragma unroll
+    for (int y = 0; y < U; ++y) {
+      if (ml[y].x == -INFINITY) {
+        if (mn == -INFINITY) sum += ml[y].y;
+        continue;
+      }
+      const float w = __builtin_amdgcn_exp2f(ml[y].x - mn);
+      if (w == 0.f) continue;  // (0 x inf)
+      sum = fmaf(w, ml[y].y, sum);
+#pragma unroll
+      for (int e = 0; e < C; ++e) acc[e] = fmaf(w, v[y][e], acc[e]);
+    }
+    m = mn;
+  }
+  __device__ __forceinline__ float scale() const { return m == -INFINITY && sum == 0.f ? 0.f : 1.f / sum; }
+  __device__ __forceinline__ float lse() const { return (m + __log2f(sum)) * kLn2; }
+};
+
 // The instance for many rows (bf16, head_dim 128): see tree_attention_wide.hip.
 constexpr int kWideRowBits = 8, kWideTileBits = 6, kWideRunBits = 8;
 size_t tree_wide_workspace();

@@ -558,14 +558,15 @@ __global__ __launch_bounds__(kThreads, NR * D * sizeof(E) <= 256 ? 2 : 1) void t
 
 // Merges the pieces of a unit that several workgroups worked on, in key order.
 // Workgroup w has the border between runs w and w + 1.  The borders inside a
-// unit share its query vectors: the first takes vectors 0, n, 2n, ... of its n
-// borders, the next 1, n + 1, ...  32 lanes hold a vector's elements.  A unit
-// of many pieces (few requests, long caches) has as many borders, and all
-// eight groups of 32 lanes take pieces of one vector in turn; with few pieces
-// a group takes a vector for itself.  The pieces' weights are known before
-// their outputs are read, so those loads do not wait for each other.
+// unit, and blockIdx.y, share its query vectors.  32 lanes hold a vector's
+// elements.  A unit of many pieces (few requests, long caches) has all eight
+// groups of 32 lanes take pieces of one vector in turn; with few pieces a
+// group takes a vector for itself.  The launch is a chain of loads from other
+// XCDs' results, about 1 us each: lengths, then a round of pieces at a time,
+// outputs and statistics together.
 constexpr int kGroups = kThreads / 32;
 constexpr int kManyPieces = 16;
+constexpr int kRound = 8;  // pieces of a round
 template <typename E, int D>
 __global__ __launch_bounds__(kThreads) void tree_combine(const SplitArgs a) {
   constexpr int C = (D + 31) / 32;  // elements a lane holds
@@ -589,77 +590,54 @@ __global__ __launch_bounds__(kThreads) void tree_combine(const SplitArgs a) {
   const bool many = pieces > kManyPieces;
   const int step = many ? kGroups : 1, x0 = many ? grp : 0;
   // (many: every group has the same vectors, so the barriers below match)
-  for (int r = w1 - 1 - w0 + (many ? 0 : borders * grp); r < vectors; r += borders * (many ? 1 : kGroups)) {
-    float M = -INFINITY, sum = 0.f, acc[C];
+  const int lot = w1 - 1 - w0 + borders * (many ? blockIdx.y : grp + kGroups * blockIdx.y);
+  for (int r = lot; r < vectors; r += borders * gridDim.y * (many ? 1 : kGroups)) {
+    Merge<C> mg;
+    for (int c = x0; c < pieces; c += kRound * step) {
+      float2 ml[kRound];
+      float v[kRound][C];
 #pragma unroll
-    for (int e = 0; e < C; ++e) acc[e] = 0.f;
-    for (int c = x0; c < pieces; c += 32 * step) {
-      const int mine = c + lane * step, cnt = min(32, (pieces - c + step - 1) / step);
-      float pm = -INFINITY, pl = 0.f;
-      const auto slot = [&](int x) { return 2 * (int64_t)(w0 + x) + (x == 0 ? first : 0); };
-      if (mine < pieces) {
-        const float2 ml = *(const float2*)(a.part_ml + ((slot(mine) << a.row_bits) + r) * 2);
-        pm = ml.x;
-        pl = ml.y;
+      for (int y = 0; y < kRound; ++y) {
+        const int x = min(c + y * step, pieces - 1);
+        const int64_t at = ((2 * (int64_t)(w0 + x) + (x == 0 ? first : 0)) << a.row_bits) + r;
+        ml[y] = *(const float2*)(a.part_ml + at * 2);
+        const float* pp = a.part + at * D + lane * C;
+#pragma unroll
+        for (int e = 0; e < C; ++e) v[y][e] = D % 32 == 0 || lane * C + e < D ? pp[e] : 0.f;
       }
-      float mx = pm;
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
-      const float mn = fmaxf(M, mx);
-      // a maximum of -inf has weight 0; where all are -inf the sums say whether
-      // a key was seen (NaN) or none (0)
-      const float w = pm == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(pm - mn);
-      float ps = pm == -INFINITY ? (mn == -INFINITY ? pl : 0.f) : w * pl;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) ps += __shfl_xor(ps, o);
-      const float back = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - mn);
-      sum = M == -INFINITY && mn != -INFINITY ? ps : fmaf(sum, mn == -INFINITY ? 1.f : back, ps);
-#pragma unroll
-      for (int e = 0; e < C; ++e) acc[e] *= back;
-      M = mn;
-#pragma unroll 8
-      for (int y = 0; y < cnt; ++y) {
-        const float wy = __shfl(w, (threadIdx.x & 32) + y);
-        const float* pp = a.part + ((slot(c + y * step) << a.row_bits) + r) * D + lane * C;
-        float v[C];
-#pragma unroll
-        for (int e = 0; e < C; ++e) v[e] = D % 32 == 0 || lane * C + e < D ? pp[e] : 0.f;
-#pragma unroll
-        for (int e = 0; e < C; ++e) acc[e] += wy != 0.f ? wy * v[e] : 0.f;
-      }
+      for (int y = 0; y < kRound; ++y)
+        if (c + y * step >= pieces) ml[y] = make_float2(-INFINITY, 0.f);
+      mg.add(ml, v);
     }
     if (many) {
       __syncthreads();  // the previous vector has been read
       if (lane == 0) {
-        s_m[grp] = M;
-        s_l[grp] = sum;
+        s_m[grp] = mg.m;
+        s_l[grp] = mg.sum;
       }
 #pragma unroll
-      for (int e = 0; e < C; ++e) s_o[grp][lane * C + e] = acc[e];
+      for (int e = 0; e < C; ++e) s_o[grp][lane * C + e] = mg.acc[e];
       __syncthreads();
-      float Mt = -INFINITY;
-#pragma unroll
-      for (int x = 0; x < kGroups; ++x) Mt = fmaxf(Mt, s_m[x]);
-      sum = 0.f;
-#pragma unroll
-      for (int e = 0; e < C; ++e) acc[e] = 0.f;
+      if (grp) continue;
+      float2 ml[kGroups];
+      float v[kGroups][C];
 #pragma unroll
       for (int x = 0; x < kGroups; ++x) {
-        const float w = s_m[x] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[x] - Mt);
-        sum += s_m[x] == -INFINITY ? (Mt == -INFINITY ? s_l[x] : 0.f) : w * s_l[x];
+        ml[x] = make_float2(s_m[x], s_l[x]);
 #pragma unroll
-        for (int e = 0; e < C; ++e) acc[e] += w != 0.f ? w * s_o[x][lane * C + e] : 0.f;
+        for (int e = 0; e < C; ++e) v[x][e] = s_o[x][lane * C + e];
       }
-      M = Mt;
-      if (grp) continue;
+      mg = Merge<C>();
+      mg.add(ml, v);
     }
     const int qv = (rt << a.row_bits) + r, i = a.group.div(qv), head = h * t.G + qv - i * t.G;
-    const float inv = sum == 0.f && M == -INFINITY ? 0.f : 1.f / sum;
+    const float inv = mg.scale();
     E* op = (E*)t.out + (q.r0 + i) * t.o_row + head * t.o_head + lane * C;
 #pragma unroll
     for (int e = 0; e < C; ++e)
-      if (D % 32 == 0 || lane * C + e < D) put_elem(op + e, acc[e] * inv);
-    if (t.lse && lane == 0) t.lse[(int64_t)(q.r0 + i) * t.Hq + head] = (M + __log2f(sum)) * kLn2;
+      if (D % 32 == 0 || lane * C + e < D) put_elem(op + e, mg.acc[e] * inv);
+    if (t.lse && lane == 0) t.lse[(int64_t)(q.r0 + i) * t.Hq + head] = mg.lse();
   }
 }
 
@@ -673,18 +651,27 @@ static bool has_instance(const Geo& g) {
   if (g.dtype == CS_BF16) return g.D == 32 || g.D == 64 || g.D == 96 || g.D == 128 || g.D == 256;
   return g.D == 16 || g.D == 32 || g.D == 64 || g.D == 128;
 }
-// Row tiles of 16, 32 or 64 query vectors: the smallest that holds the rows
-// that a request is expected to have.
+static bool wide_type(const Geo& g) { return g.dtype == CS_BF16 && g.D == 128; }
+// Row tiles of 16, 32 or 64 query vectors.  A larger one reads the keys fewer
+// times and leaves fewer wavefronts to a SIMD; with rows of 256 bytes and more
+// 64 do not fit the registers.  Measured (us): 65,000 tokens, 8 query heads a KV
+// head, float32 x 128, 17 rows: 169 / 114 / 388 with 16 / 32 / 64; bf16 x 64, 64
+// rows: 93 / 79 / 66, but 4 requests of up to 4,096 tokens, 17 rows: 14 / 14 / 19.
 static int row_groups(const Geo& g, const cs_batch& b) {
   const int64_t rows = b.max_rows > 0 ? b.max_rows : b.n_rows;
   const int64_t qv = rows * g.G;
-  return qv <= 16 ? 1 : qv <= 32 ? 2 : 4;
+  if (qv <= (wide_type(g) ? 32 : 16) || g.D > 128) return 1;
+  return qv <= 256 || g.D * g.esize >= 256 ? 2 : 4;
 }
 
-// Whether the kernel for many rows takes the batch (where its pointers are aligned).
+// Whether the kernel for many rows takes the batch (where its pointers are
+// aligned).  Measured (us, with 16 query vectors a row tile / that kernel), 8
+// query heads a KV head: 65,000 tokens, 4 rows 27 / 22, 16 rows 79 / 23; 16
+// requests of up to 4,000 tokens, 4 rows 20 / 20, 16 rows 31 / 21; 8,000 tokens, 4
+// rows 14 / 17, 16 rows 16 / 17.
 static bool wide(const Geo& g, const cs_batch& b) {
   const int64_t rows = b.max_rows > 0 ? b.max_rows : b.n_rows;
-  return g.dtype == CS_BF16 && g.D == 128 && g.T % 16 == 0 && rows * g.G > 64;
+  return wide_type(g) && g.T % 16 == 0 && rows * g.G > 32;
 }
 
 size_t tree_attend_workspace(const Geo& g, const cs_batch& b) {
@@ -701,13 +688,15 @@ static void run_split(const SplitArgs& a, hipStream_t s) {
     CS_LAUNCH(tr, (tree_attend<E, D, NR>), dim3(kRuns), dim3(kThreads), 0, s, a);
   }
   TraceScope tr("tree_combine", s);
-  CS_LAUNCH(tr, (tree_combine<E, D>), dim3(kRuns - 1), dim3(kThreads), 0, s, a);
+  CS_LAUNCH(tr, (tree_combine<E, D>), dim3(kRuns - 1, 2 * NR), dim3(kThreads), 0, s, a);
 }
 template <typename E, int D>
 static void run_split(const SplitArgs& a, int nr, hipStream_t s) {
-  if (nr == 1) run_split<E, D, 1>(a, s);
-  else if (nr == 2) run_split<E, D, 2>(a, s);
-  else run_split<E, D, 4>(a, s);
+  if constexpr (D * sizeof(E) < 256)
+    if (nr == 4) return run_split<E, D, 4>(a, s);
+  if constexpr (D <= 128)
+    if (nr == 2) return run_split<E, D, 2>(a, s);
+  run_split<E, D, 1>(a, s);
 }
 
 cs_status launch_tree_attend(const Geo& g, const cs_page_pool& pool, int layer, const cs_batch& b, const cs_rows& q,

@@ -14,8 +14,12 @@
 // of no page of the pool, read as zeros.
 //
 // The work is cut as in the kernel for few rows (equal runs of key tiles, one
-// run for each of 256 workgroups, one workgroup per CU); pieces of a unit
-// leave float32 partials in the accumulators' own layout.
+// run for each of 256 workgroups, one workgroup per CU).  A piece of a unit
+// leaves its outputs, in the accumulators' own layout, divided by their sum and
+// by 2^e, so that a query vector's largest lies in [0.5, 1), and rounded to fp16:
+// 11 bits relative to that largest element, a quarter of the output's own
+// rounding, for half the bytes of float32 (a launch of 256 pieces leaves 17 MB
+// and the merge reads them: see tree_combine_wide).
 #include <math.h>
 
 #include <type_traits>
@@ -31,7 +35,8 @@ constexpr int kRow = 256;                // bytes of a K/V row
 constexpr int kHiLds = 65536;            // LDS bytes below the K ring (the V ring)
 constexpr float kRescaleLog2 = 5.f;      // growth of the running maximum before the accumulators are rescaled
 constexpr int kWideRuns = 1 << kWideRunBits;
-constexpr int kPartFloats = 256 * 128;   // a partial's outputs
+constexpr int kPartHalfs = 256 * 128;    // a partial's outputs
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 typedef __attribute__((address_space(3))) void lds_void;
@@ -154,25 +159,35 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
     }
     bad = __syncthreads_or(bad);  // (the ring is free as well: every wavefront has left the previous piece)
 
-    // this wavefront's 8 keys of tile i: their page, and the loads into a ring slot
+    // this wavefront's 8 keys of tile i: their page, and the loads into a ring
+    // slot (what they need of the arguments stays in scalar registers: read
+    // again in every step it would hold the step up)
     int page_next = 0;
-    auto find_page = [&](int i) {
+    FastDiv page;
+    scalar_ptr table;
+    const char *k_plane, *v_plane;
+    int64_t page_bytes;
+    int n_pages;
+    {
       const SplitArgs A = args();
-      const scalar_ptr tb = (scalar_ptr)(uint64_t)(A.t.table + (int64_t)b * A.t.max_blocks);
-      if (q.len > 0) page_next = tb[A.t.page.div(min(key_begin + i * kKT + 8 * wave, q.len - 1))];
+      page = A.t.page;
+      table = (scalar_ptr)(uint64_t)(A.t.table + (int64_t)b * A.t.max_blocks);
+      const int64_t plane = ((int64_t)A.t.layer * A.t.Hkv + h) * page.d * kRow;
+      k_plane = A.t.pool.k + plane;
+      v_plane = A.t.pool.v + plane;
+      page_bytes = A.t.pool.page_bytes;
+      n_pages = A.t.pool.n_pages;
+    }
+    const int last_key = q.len - 1, key_wave = key_begin + 8 * wave;
+    auto find_page = [&](int i) {
+      if (last_key >= 0) page_next = table[page.div(min(key_wave + i * kKT, last_key))];
     };
     auto fetch = [&](int i, char* Kd, char* Vd) {
-      const SplitArgs A = args();
-      const int key = key_begin + i * kKT + 8 * wave;
-      const bool ok = i < n_kt && key < q.len && page_next >= 0 && page_next < A.t.pool.n_pages;
-      int64_t at = 0;
-      int bytes = 0;
-      if (ok) {
-        at = page_next * A.t.pool.page_bytes +
-             (((int64_t)A.t.layer * A.t.Hkv + h) * A.t.page.d + key - A.t.page.div(key) * A.t.page.d) * kRow;
-        bytes = min(q.len - key, 8) * kRow;
-      }
-      const auto rk = rows_rsrc(A.t.pool.k + at, bytes), rv = rows_rsrc(A.t.pool.v + at, bytes);
+      const int key = key_wave + i * kKT;
+      const bool ok = i < n_kt && key <= last_key && (unsigned)page_next < (unsigned)n_pages;
+      const int64_t at = page_next * page_bytes + (int64_t)(key - page.div(key) * page.d) * kRow;
+      const int bytes = ok ? min(last_key + 1 - key, 8) * kRow : 0;  // (no bytes: no address is used)
+      const auto rk = rows_rsrc(k_plane + at, bytes), rv = rows_rsrc(v_plane + at, bytes);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const int r0 = 8 * wave + 4 * j;
@@ -431,13 +446,28 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
       }
     } else {
       const int64_t slot = 2 * (int64_t)blockIdx.x + (first_seg ? 0 : 1);
-      if (hi == 0) *(float2*)(A.part_ml + (slot * 256 + 32 * wave + ql) * 2) = make_float2(m_use, lt);
-      float* pp = A.part + slot * kPartFloats + wave * (16 * 256) + lane * 4;
+      float amax = 0.f;
 #pragma unroll
       for (int d = 0; d < 4; ++d)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          *(f32x4*)(pp + (4 * d + r) * 256) = f32x4{o[d][4 * r], o[d][4 * r + 1], o[d][4 * r + 2], o[d][4 * r + 3]};
+        for (int r = 0; r < 16; ++r) amax = fmaxf(amax, fabsf(o[d][r]) < INFINITY ? fabsf(o[d][r]) : 0.f);
+      const float inv = lt > 0.f ? 1.f / lt : 1.f;  // (no key seen: zeros; NaN stays)
+      amax = pair_max(amax) * inv;
+      const int e = amax > 0.f ? min(max(__builtin_amdgcn_frexp_expf(amax), -100), 100) : 0;  // 2^-e stays normal
+      const float by = inv * __builtin_ldexpf(1.f, -e);
+      if (hi == 0)
+        *(float4*)(A.part_ml + (slot * 256 + 32 * wave + ql) * 4) =
+            make_float4(m_use, lt, __builtin_ldexpf(lt > 0.f ? lt : 1.f, e), 0.f);
+      _Float16* pp = (_Float16*)A.part + slot * kPartHalfs + wave * (8 * 512) + lane * 8;
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          f16x8 w;
+#pragma unroll
+          for (int x = 0; x < 8; ++x) w[x] = (_Float16)(o[d][8 * r + x] * by);
+          *(f16x8*)(pp + (2 * d + r) * 512) = w;
+        }
     }
     first_seg = false;
     left -= seg;
@@ -446,12 +476,16 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
   }
 }
 
-// Merges the pieces of a unit, in key order.  A wavefront takes the same 16
-// bytes of 32 query vectors' halves (one store of a piece's wavefront: 1 KB in
-// a row) through all pieces; the unit's 128 such strips are shared by the
-// workgroups of the borders inside it.
+// Merges the pieces of a unit, in key order.  A strip is what one store of a
+// wavefront left, 1 KB in a row: 8 elements of 32 query vectors' halves.  The
+// unit's 64 strips are shared by the workgroups of the borders inside it,
+// blockIdx.y among them.  With few pieces a wavefront takes a strip through all
+// of them; with many, four wavefronts take the pieces of a strip in turn.
 constexpr int kStripThreads = 256;
+constexpr int kStripShare = 4;
+constexpr int kRound = 8;
 __global__ __launch_bounds__(kStripThreads) void tree_combine_wide(const SplitArgs a) {
+  __shared__ float s_acc[4][8][64], s_m[4][64], s_l[4][64];
   const TreeArgs& t = a.t;
   const int w1 = blockIdx.x + 1;
   Run run;
@@ -465,61 +499,69 @@ __global__ __launch_bounds__(kStripThreads) void tree_combine_wide(const SplitAr
   const int w0 = quotient(unit0, len), w_last = quotient(unit0 + ntile - 1, len);
   const int pieces = w_last - w0 + 1, borders = pieces - 1;
   const int first = w0 * len < unit0 ? 1 : 0;
-  const int h = u / nrt, rt = u - h * nrt, vectors = q.n * t.G;
-  const int lane = threadIdx.x & 63, ql = lane & 31, hi = lane >> 5;
-  for (int strip = (w1 - 1 - w0) * 4 + uniform(threadIdx.x >> 6); strip < 128; strip += borders * 4) {
-    const int wave = strip >> 4, c = strip & 15, qv = rt * 256 + 32 * wave + ql;
-    if (rt * 256 + 32 * wave >= vectors) break;  // (strips ascend)
-    float M = -INFINITY, sum = 0.f;
-    f32x4 acc = f32x4{};
-    constexpr int U = 8;
-    for (int x = 0; x < pieces; x += U) {
-      float2 ml[U];
-      f32x4 v[U];
+  const int h = u / nrt, rt = u - h * nrt, vectors = min(256, q.n * t.G - rt * 256);
+  const int lane = threadIdx.x & 63, ql = lane & 31, hi = lane >> 5, grp = uniform(threadIdx.x >> 6);
+  const bool many = pieces > kRound;
+  const int step = many ? 4 : 1, strips = (vectors + 31) / 32 * 8;
+  const int lot = (w1 - 1 - w0) * kStripShare + blockIdx.y;
+  for (int strip = many ? lot : lot * 4 + grp; strip < strips; strip += borders * kStripShare * (many ? 1 : 4)) {
+    const int wave = strip >> 3, c = strip & 7, r = 32 * wave + ql;
+    Merge<8> mg;
+    for (int x0 = many ? grp : 0; x0 < pieces; x0 += kRound * step) {
+      float4 st[kRound];
+      f16x8 v16[kRound];
 #pragma unroll
-      for (int y = 0; y < U; ++y) {
-        const int p = min(x + y, pieces - 1);
-        const int64_t slot = 2 * (int64_t)(w0 + p) + (p == 0 ? first : 0);
-        ml[y] = *(const float2*)(a.part_ml + (slot * 256 + 32 * wave + ql) * 2);
-        v[y] = *(const f32x4*)(a.part + slot * kPartFloats + strip * 256 + lane * 4);
+      for (int y = 0; y < kRound; ++y) {
+        const int x = min(x0 + y * step, pieces - 1);
+        const int64_t slot = 2 * (int64_t)(w0 + x) + (x == 0 ? first : 0);
+        st[y] = *(const float4*)(a.part_ml + (slot * 256 + r) * 4);
+        v16[y] = *(const f16x8*)((const _Float16*)a.part + slot * kPartHalfs + strip * 512 + lane * 8);
       }
-      float mn = M;
+      float2 ml[kRound];
+      float v[kRound][8];
 #pragma unroll
-      for (int y = 0; y < U; ++y) mn = fmaxf(mn, x + y < pieces ? ml[y].x : -INFINITY);
-      if (M != -INFINITY) {
-        const float back = __builtin_amdgcn_exp2f(M - mn);
-        sum *= back;
-        acc *= back;
-      } else if (mn != -INFINITY) {
-        sum = 0.f;  // (pieces of scores of -inf alone do not count beside others)
+      for (int y = 0; y < kRound; ++y) {
+        ml[y] = x0 + y * step < pieces ? make_float2(st[y].x, st[y].y) : make_float2(-INFINITY, 0.f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[y][e] = (float)v16[y][e] * st[y].z;
       }
-#pragma unroll
-      for (int y = 0; y < U; ++y) {
-        if (x + y >= pieces) continue;
-        if (ml[y].x == -INFINITY) {
-          if (mn == -INFINITY) sum += ml[y].y;
-          continue;
-        }
-        const float w = __builtin_amdgcn_exp2f(ml[y].x - mn);
-        sum = fmaf(w, ml[y].y, sum);
-        if (w != 0.f)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[e] = fmaf(w, v[y][e], acc[e]);
-      }
-      M = mn;
+      mg.add(ml, v);
     }
-    if (qv >= vectors) continue;
-    const int i = a.group.div(qv), head = h * t.G + qv - i * t.G;
-    const float inv = M == -INFINITY && sum == 0.f ? 0.f : 1.f / sum;
-    u32x2 w;
-    w[0] = pack_bf16x2(acc[0] * inv, acc[1] * inv);
-    w[1] = pack_bf16x2(acc[2] * inv, acc[3] * inv);
-    *(u32x2*)((uint16_t*)t.out + (int64_t)(q.r0 + i) * t.o_row + head * t.o_head + 32 * (c >> 2) + 8 * (c & 3) + 4 * hi) = w;
-    if (t.lse && c == 0 && hi == 0) t.lse[(int64_t)(q.r0 + i) * t.Hq + head] = (M + __log2f(sum)) * kLn2;
+    if (many) {
+      __syncthreads();  // the previous strip has been read
+      s_m[grp][lane] = mg.m;
+      s_l[grp][lane] = mg.sum;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s_acc[grp][e][lane] = mg.acc[e];
+      __syncthreads();
+      if (grp) continue;
+      float2 ml[4];
+      float v[4][8];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        ml[x] = make_float2(s_m[x][lane], s_l[x][lane]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[x][e] = s_acc[x][e][lane];
+      }
+      mg = Merge<8>();
+      mg.add(ml, v);
+    }
+    if (r >= vectors) continue;
+    const int qv = rt * 256 + r, i = a.group.div(qv), head = h * t.G + qv - i * t.G;
+    const float inv = mg.scale();
+    uint16_t* op = (uint16_t*)t.out + (int64_t)(q.r0 + i) * t.o_row + head * t.o_head + 16 * c + 4 * hi;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {  // elements 4x .. 4x + 3 are dims 16c + 8x + 4hi ..
+      u32x2 w;
+      w[0] = pack_bf16x2(mg.acc[4 * x] * inv, mg.acc[4 * x + 1] * inv);
+      w[1] = pack_bf16x2(mg.acc[4 * x + 2] * inv, mg.acc[4 * x + 3] * inv);
+      *(u32x2*)(op + 8 * x) = w;
+    }
+    if (t.lse && c == 0 && hi == 0) t.lse[(int64_t)(q.r0 + i) * t.Hq + head] = mg.lse();
   }
 }
 
-size_t tree_wide_workspace() { return 2 * (size_t)kWideRuns * (kPartFloats + 2 * 256) * sizeof(float) + 512; }
+size_t tree_wide_workspace() { return 2 * (size_t)kWideRuns * (kPartHalfs * sizeof(_Float16) + 4 * 256 * sizeof(float)) + 512; }
 
 void launch_tree_wide(SplitArgs a, void* ws, hipStream_t s) {
   a.row_bits = kWideRowBits;
@@ -527,13 +569,13 @@ void launch_tree_wide(SplitArgs a, void* ws, hipStream_t s) {
   a.run_bits = kWideRunBits;
   a.min_tiles = 4;
   a.part = (float*)(((uintptr_t)ws + 255) & ~(uintptr_t)255);
-  a.part_ml = a.part + 2 * (size_t)kWideRuns * kPartFloats;
+  a.part_ml = a.part + 2 * (size_t)kWideRuns * kPartHalfs / 2;
   {
     TraceScope tr("tree_attend_wide", s);
     CS_LAUNCH(tr, tree_attend_wide, dim3(kWideRuns), dim3(kWideThreads), 0, s, a);
   }
   TraceScope tr("tree_combine_wide", s);
-  CS_LAUNCH(tr, tree_combine_wide, dim3(kWideRuns - 1), dim3(kStripThreads), 0, s, a);
+  CS_LAUNCH(tr, tree_combine_wide, dim3(kWideRuns - 1, kStripShare), dim3(kStripThreads), 0, s, a);
 }
 
 }  // namespace cs
