@@ -164,7 +164,7 @@ __device__ __forceinline__ float group_sum(float x) {
 }
 
 template <typename E, int D, int NR>
-__global__ __launch_bounds__(kThreads, NR * D * sizeof(E) <= 256 ? 2 : 1) void tree_attend(const SplitArgs a) {
+__global__ __launch_bounds__(kThreads, NR * D * sizeof(E) <= 256 ? 2 : 1) void tree_attend(const SplitArgs) {
   constexpr bool kBf16 = sizeof(E) == 2;
   constexpr int SUB = kBf16 ? 2 : 1;             // 16-key pieces of a tile
   constexpr int KT = 16 * SUB;
@@ -181,17 +181,27 @@ __global__ __launch_bounds__(kThreads, NR * D * sizeof(E) <= 256 ? 2 : 1) void t
 
   __shared__ float s_o[kWaves * 16 * kPad];
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
   const int ln = lane & 15, lg = lane >> 4;
+  // The arguments are read where they are used: a launch is short, and what it
+  // spends on moving arguments in and out of scalar registers, and on fetching
+  // the instructions that do, is part of its latency.
+  typedef const __attribute__((address_space(4))) SplitArgs* ArgPtr;
+  const ArgPtr argp = (ArgPtr)__builtin_amdgcn_kernarg_segment_ptr();
+  auto args = [&]() -> SplitArgs {
+    ArgPtr p = argp;
+    asm volatile("" : "+s"(p));
+    return *(const SplitArgs*)p;
+  };
   Run run;
-  if (!find_run(a, blockIdx.x, &run)) return;
-  const TreeArgs& t = a.t;
+  if (!find_run(args(), blockIdx.x, &run)) return;
   int64_t left = run.end - run.begin, off = run.off;
   int b = run.b;
-  const float sc = t.scale * kLog2e;
   bool first_seg = true;
 
   while (left > 0) {
+    const SplitArgs a = args();
+    const TreeArgs& t = a.t;
     const Request q = load_request_scalar(t, b);
     int nrt, ntile;
     unit_sizes(a, q, &nrt, &ntile);
@@ -204,60 +214,56 @@ __global__ __launch_bounds__(kThreads, NR * D * sizeof(E) <= 256 ? 2 : 1) void t
     const int u = uniform(unit_at(off, ntile, &t0));
     t0 = uniform(t0);
     const int seg = (int)min(left, (int64_t)(ntile - t0));
-    const int h = uniform(u / nrt), rt = u - h * nrt;
-    const bool whole = seg == ntile;
+    const int h = nrt == 1 ? u : uniform(u / nrt), rt = u - h * nrt;
+    const int vectors = q.n * t.G;
     // rows see no key behind their own without a mask, so later tiles are left out
-    const int i_last = a.group.div(min(rt * RT + RT - 1, q.n * t.G - 1));
+    const int i_last = a.group.div(min(rt * RT + RT, vectors) - 1);
     const int key_end = t.mask ? q.len : min(q.len, q.cached + i_last + 1);
     const int t_end = min(t0 + seg, (key_end + KT - 1) / KT);
+    const int t_full = min(q.cached, q.len) / KT;  // tiles before it: every row sees every key
 
     Words<16> qf[NR][KS];
     int row[NR];  // the lane's row in the request, per 16 query vectors
 #pragma unroll
     for (int x = 0; x < NR; ++x) {
-      const int qv = rt * RT + 16 * x + ln;
-      const bool valid = qv < q.n * t.G;
-      const int i = valid ? a.group.div(qv) : q.n - 1;
+      const int qv = min(rt * RT + 16 * x + ln, vectors - 1), i = a.group.div(qv);
       row[x] = i;
-      const char* qp = (const char*)t.q + ((int64_t)(q.r0 + i) * t.q_row + (h * t.G + (valid ? qv - i * t.G : 0)) * t.q_head) * (int)sizeof(E);
+      const char* qp = (const char*)t.q + ((int64_t)(q.r0 + i) * t.q_row + (h * t.G + qv - i * t.G) * t.q_head) * (int)sizeof(E);
 #pragma unroll
       for (int k = 0; k < KS; ++k) qf[x][k] = *(const Words<16>*)(qp + 64 * k + 16 * lg);
     }
 
-    const int32_t* table = t.table + (int64_t)b * t.max_blocks;
-    const int64_t plane = ((int64_t)t.layer * t.Hkv + h) * t.page.d * kRowB;
-    Words<16> kf[SUB][KS];
-    Words<VB> vf[SUB * 4][NB];
-    bool have[SUB];  // the 16 keys lie in a page of the pool
     // Where the 16-key pieces of a tile lie: 16 rows of a page (pages are
     // multiples of 16 tokens), as many of them as the request has; none behind
     // the request's or the run's end.  The page numbers come through the scalar
     // cache, a tile ahead of the loads that need them, so that nothing waits
     // for the values in flight.
-    const scalar_ptr pages = (scalar_ptr)(uint64_t)table;
+    const scalar_ptr pages = (scalar_ptr)(uint64_t)(t.table + (int64_t)b * t.max_blocks);
+    const FastDiv page_div = t.page;
+    const int64_t plane = ((int64_t)t.layer * t.Hkv + h) * page_div.d * kRowB, page_bytes = t.pool.page_bytes;
+    const char *k_plane = t.pool.k + plane, *v_plane = t.pool.v + plane;
+    const int n_pages = t.pool.n_pages;
+    Words<16> kf[SUB][KS];
+    Words<VB> vf[SUB * 4][NB];
     int64_t at[SUB];
     int bytes[SUB], page[SUB];
-    bool ok[SUB];
     auto fetch_pages = [&](int tile) {
 #pragma unroll
-      for (int s = 0; s < SUB; ++s) {
-        const int key = min(tile, t_end - 1) * KT + 16 * s;
-        page[s] = pages[t.page.div(min(key, q.len - 1))];
-      }
+      for (int s = 0; s < SUB; ++s) page[s] = pages[page_div.div(min(min(tile, t_end - 1) * KT + 16 * s, q.len - 1))];
     };
     auto places = [&](int tile) {
 #pragma unroll
       for (int s = 0; s < SUB; ++s) {
         const int key = tile * KT + 16 * s;
-        ok[s] = tile < t_end && key < q.len && page[s] >= 0 && page[s] < t.pool.n_pages;
-        at[s] = ok[s] ? page[s] * t.pool.page_bytes + plane + (int64_t)(key - t.page.div(key) * t.page.d) * kRowB : 0;
-        bytes[s] = ok[s] ? min(q.len - key, 16) * kRowB : 0;
+        at[s] = page[s] * page_bytes + (int64_t)(key - page_div.div(key) * page_div.d) * kRowB;
+        // (no bytes: no address is used)
+        bytes[s] = tile < t_end && key < q.len && (unsigned)page[s] < (unsigned)n_pages ? min(q.len - key, 16) * kRowB : 0;
       }
     };
     auto load_k = [&]() {
 #pragma unroll
       for (int s = 0; s < SUB; ++s) {
-        const auto r = rows_rsrc(t.pool.k + at[s], bytes[s]);
+        const auto r = rows_rsrc(k_plane + at[s], bytes[s]);
 #pragma unroll
         for (int k = 0; k < KS; ++k) kf[s][k] = load_words<16>(r, ln * kRowB + 64 * k + 16 * lg);
       }
@@ -265,7 +271,7 @@ __global__ __launch_bounds__(kThreads, NR * D * sizeof(E) <= 256 ? 2 : 1) void t
     auto load_v = [&]() {
 #pragma unroll
       for (int s = 0; s < SUB; ++s) {
-        const auto r = rows_rsrc(t.pool.v + at[s], bytes[s]);
+        const auto r = rows_rsrc(v_plane + at[s], bytes[s]);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -273,6 +279,7 @@ __global__ __launch_bounds__(kThreads, NR * D * sizeof(E) <= 256 ? 2 : 1) void t
       }
     };
 
+    const float sc = t.scale * kLog2e;
     f32x4 o[NR][NO];
     float m[NR], l[NR];
     bool seen[NR];  // some key was visible
@@ -285,6 +292,44 @@ __global__ __launch_bounds__(kThreads, NR * D * sizeof(E) <= 256 ? 2 : 1) void t
       for (int e = 0; e < NO; ++e) o[x][e] = f32x4{};
     }
 
+    // value(j, n, w): word w of key j's block n; weight(x, j): of query vector and key
+    auto pv = [&](auto value, auto weight, auto add) {
+      if constexpr (kBf16) {
+        bf16x8 pb[NR];
+#pragma unroll
+        for (int x = 0; x < NR; ++x)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) pb[x][j] = (__bf16)weight(x, j);
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int e = 0; e < VW; ++e) {
+            u32x4 va;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              va[j] = __builtin_amdgcn_perm(value(2 * j + 1, n, e / 2), value(2 * j, n, e / 2), e & 1 ? 0x07060302 : 0x05040100);
+#pragma unroll
+            for (int x = 0; x < NR; ++x)
+              add(x, n * VW + e, [&](f32x4 c) {
+                return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va), pb[x], c, 0, 0, 0);
+              });
+          }
+      } else {
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int e = 0; e < VW; ++e)
+#pragma unroll
+            for (int x = 0; x < NR; ++x)
+              add(x, n * VW + e, [&](f32x4 c) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                  c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(value(j, n, e)), weight(x, j), c, 0, 0, 0);
+                return c;
+              });
+      }
+    };
+
     int tile = t0 + wave;
     if (tile < t_end && q.len > 0) {
       fetch_pages(tile);
@@ -293,8 +338,11 @@ __global__ __launch_bounds__(kThreads, NR * D * sizeof(E) <= 256 ? 2 : 1) void t
       load_v();
       fetch_pages(tile + kWaves);
     }
-    auto step = [&](auto masked) {
-      constexpr bool kMasked = decltype(masked)::value;
+    // One body for every tile: the masked tiles' extra work is behind a branch,
+    // so that their first one finds its instructions fetched (with bodies of
+    // their own it cost 3 us).
+#pragma unroll 1
+    for (; tile < t_end; tile += kWaves) {
       const int key0 = tile * KT;
       f32x4 s[NR][SUB];
 #pragma unroll
@@ -315,30 +363,40 @@ __global__ __launch_bounds__(kThreads, NR * D * sizeof(E) <= 256 ? 2 : 1) void t
             }
           }
         }
+      bool have[SUB], some = false;  // the 16 keys lie in a page of the pool
 #pragma unroll
-      for (int y = 0; y < SUB; ++y) have[y] = ok[y];
+      for (int y = 0; y < SUB; ++y) {
+        have[y] = bytes[y] != 0;
+        some = some || have[y];
+      }
       places(tile + kWaves);
       load_k();
       fetch_pages(tile + 2 * kWaves);
 
-      uint32_t vis[NR];  // bit of key 16 y + 4 lg + i at 16 y + 4 lg + i
-      if constexpr (kMasked) {
+      float p[NR][NS];
+#pragma unroll
+      for (int x = 0; x < NR; ++x)
+#pragma unroll
+        for (int y = 0; y < SUB; ++y)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) p[x][4 * y + i] = fmaf(s[x][y][i], sc, have[y] ? 0.f : -INFINITY);
+      const bool masked = tile >= t_full;
+      uint32_t vis[NR];  // bit 16 y + i: key 16 y + 4 lg + i
+      if (masked) {
+        const SplitArgs A = args();
         uint32_t there = 0;  // keys of the request that lie in the pool
 #pragma unroll
-        for (int y = 0; y < SUB; ++y) {
-          const int n = min(max(q.len - key0 - 16 * y, 0), 16);
-          if (have[y]) there |= ((1u << n) - 1) << (16 * y);
-        }
-        const int w0 = key0 - q.cached;  // new row of the tile's first key
+        for (int y = 0; y < SUB; ++y)
+          if (have[y]) there |= ((1u << min(max(q.len - key0 - 16 * y, 0), 16)) - 1) << (16 * y);
+        const int w0 = key0 - q.cached, w = max(w0, 0);  // new row of the tile's first key
 #pragma unroll
         for (int x = 0; x < NR; ++x) {
-          uint64_t bits = 0;  // visible rows from max(w0, 0) on
-          const int w = max(w0, 0);
-          if (t.mask) {
-            const unsigned long long* mk = t.mask + (int64_t)(q.r0 + row[x]) * t.words;
+          uint64_t bits = 0;  // visible rows from w on
+          if (A.t.mask) {
+            const unsigned long long* mk = A.t.mask + (int64_t)(q.r0 + row[x]) * A.t.words;
             const int j = w >> 6, sft = w & 63;
-            if (w0 + KT > 0 && j < t.words) bits = mk[j] >> sft;
-            if (w0 + KT > 0 && sft && j + 1 < t.words) bits |= mk[j + 1] << (64 - sft);
+            if (w0 > -KT && j < A.t.words) bits = mk[j] >> sft;
+            if (w0 > -KT && sft && j + 1 < A.t.words) bits |= mk[j + 1] << (64 - sft);
           } else {
             const int n = row[x] - w + 1;
             bits = n >= 64 ? ~0ull : n > 0 ? (1ull << n) - 1 : 0ull;
@@ -346,29 +404,21 @@ __global__ __launch_bounds__(kThreads, NR * D * sizeof(E) <= 256 ? 2 : 1) void t
           if (w0 < 0) bits = -w0 >= 64 ? ~0ull : bits << -w0 | ((1ull << -w0) - 1);
           vis[x] = (uint32_t)bits & there;
           seen[x] = seen[x] || vis[x];
+          vis[x] >>= 4 * lg;
+#pragma unroll
+          for (int j = 0; j < NS; ++j)
+            if (!(vis[x] >> (16 * (j >> 2) + (j & 3)) & 1)) p[x][j] = -INFINITY;
         }
       } else {
-        bool some = false;
-#pragma unroll
-        for (int y = 0; y < SUB; ++y) some = some || have[y];
 #pragma unroll
         for (int x = 0; x < NR; ++x) seen[x] = seen[x] || some;
       }
 
-      float p[NR][NS];
 #pragma unroll
       for (int x = 0; x < NR; ++x) {
-        float mx = -INFINITY;
+        float mx = p[x][0];
 #pragma unroll
-        for (int y = 0; y < SUB; ++y)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            // (keys in no page of the pool: not seen)
-            float v = kMasked ? s[x][y][i] * sc : fmaf(s[x][y][i], sc, have[y] ? 0.f : -INFINITY);
-            if constexpr (kMasked) v = (vis[x] >> (16 * y + 4 * lg + i)) & 1 ? v : -INFINITY;
-            p[x][4 * y + i] = v;
-            mx = fmaxf(mx, v);
-          }
+        for (int j = 1; j < NS; ++j) mx = fmaxf(mx, p[x][j]);
         mx = group_max(mx);
         const bool grow = mx > m[x] + kRescaleLog2;
         if (__ballot(grow)) {
@@ -388,9 +438,10 @@ __global__ __launch_bounds__(kThreads, NR * D * sizeof(E) <= 256 ? 2 : 1) void t
       }
 
       // Values that are not finite must not reach rows that do not see them
-      // (0 x inf): rare, and only among the step's own rows.
-      uint32_t odd = 0;  // the exponents' carries: all ones
-      if constexpr (kMasked) {
+      // (0 x inf): rare, and only among the step's own rows.  0 x value is NaN
+      // where there is one.
+      if (masked) {
+        float odd = 0.f;
 #pragma unroll
         for (int j = 0; j < SUB * 4; ++j)
 #pragma unroll
@@ -398,155 +449,108 @@ __global__ __launch_bounds__(kThreads, NR * D * sizeof(E) <= 256 ? 2 : 1) void t
 #pragma unroll
             for (int w = 0; w < VB / 4; ++w) {
               const uint32_t v = vf[j][n].w[w];
-              odd |= kBf16 ? (v & 0x7f807f80u) + 0x00800080u : (v & 0x7f800000u) + 0x00800000u;
+              if constexpr (kBf16)
+                odd = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, v), bf16x2{(__bf16)0.f, (__bf16)0.f}, odd, false);
+              else
+                odd = fmaf(__uint_as_float(v), 0.f, odd);
             }
-      }
-      auto pv = [&](auto value, auto weight, auto add) {
-        // value(j, n, w): word w of key j's block n; weight(x, j): of query vector and key
-        if constexpr (kBf16) {
-          bf16x8 pb[NR];
-#pragma unroll
-          for (int x = 0; x < NR; ++x)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) pb[x][j] = (__bf16)weight(x, j);
-#pragma unroll
-          for (int n = 0; n < NB; ++n)
-#pragma unroll
-            for (int e = 0; e < VW; ++e) {
-              u32x4 va;
-#pragma unroll
-              for (int j = 0; j < 4; ++j)
-                va[j] = __builtin_amdgcn_perm(value(2 * j + 1, n, e / 2), value(2 * j, n, e / 2), e & 1 ? 0x07060302 : 0x05040100);
-#pragma unroll
-              for (int x = 0; x < NR; ++x)
-                add(x, n * VW + e, [&](f32x4 c) {
-                  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va), pb[x], c, 0, 0, 0);
-                });
-            }
-        } else {
-#pragma unroll
-          for (int n = 0; n < NB; ++n)
-#pragma unroll
-            for (int e = 0; e < VW; ++e)
-#pragma unroll
-              for (int x = 0; x < NR; ++x)
-                add(x, n * VW + e, [&](f32x4 c) {
-#pragma unroll
-                  for (int j = 0; j < 4; ++j)
-                    c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(value(j, n, e)), weight(x, j), c, 0, 0, 0);
-                  return c;
-                });
-        }
-      };
-      if (kMasked && __ballot(odd & (kBf16 ? 0x80008000u : 0x80000000u))) {
-        // How many values of +inf (or NaN), and of -inf (or NaN), each output
-        // element gets from keys that its row sees; those give it the infinity,
-        // both of them NaN.  The values themselves become zero.
+        if (__ballot(odd != odd)) {
+          // How many values of +inf (or NaN), and of -inf (or NaN), each output
+          // element gets from keys that its row sees; those give it the infinity,
+          // both of them NaN.  The values themselves become zero.
 #pragma unroll 1
-        for (int sign = 0; sign < 2; ++sign) {
-          auto flag16 = [&](uint32_t v) -> uint32_t {  // 1.0 in bf16 where the element counts
-            const bool nan = (v & 0x7f80u) == 0x7f80u && (v & 0x7fu);
-            return nan || (v & 0xffffu) == (sign ? 0xff80u : 0x7f80u) ? 0x3f80u : 0u;
-          };
-          auto flag = [&](uint32_t v) -> uint32_t {
-            if constexpr (kBf16) return flag16(v) | flag16(v >> 16) << 16;
-            const bool nan = (v & 0x7f800000u) == 0x7f800000u && (v & 0x7fffffu);
-            return nan || v == (sign ? 0xff800000u : 0x7f800000u) ? 0x3f800000u : 0u;
-          };
-          pv([&](int j, int n, int w) { return flag(vf[j][n].w[w]); },
-             [&](int x, int j) { return (vis[x] >> (16 * (j >> 2) + 4 * lg + (j & 3))) & 1 ? 1.f : 0.f; },
-             [&](int x, int e, auto mul) {
-               const f32x4 c = mul(f32x4{});
+          for (int sign = 0; sign < 2; ++sign) {
+            auto flag16 = [&](uint32_t v) -> uint32_t {  // 1.0 in bf16 where the element counts
+              const bool nan = (v & 0x7f80u) == 0x7f80u && (v & 0x7fu);
+              return nan || (v & 0xffffu) == (sign ? 0xff80u : 0x7f80u) ? 0x3f80u : 0u;
+            };
+            auto flag = [&](uint32_t v) -> uint32_t {
+              if constexpr (kBf16) return flag16(v) | flag16(v >> 16) << 16;
+              const bool nan = (v & 0x7f800000u) == 0x7f800000u && (v & 0x7fffffu);
+              return nan || v == (sign ? 0xff800000u : 0x7f800000u) ? 0x3f800000u : 0u;
+            };
+            pv([&](int j, int n, int w) { return flag(vf[j][n].w[w]); },
+               [&](int x, int j) { return vis[x] >> (16 * (j >> 2) + (j & 3)) & 1 ? 1.f : 0.f; },
+               [&](int x, int e, auto mul) {
+                 const f32x4 c = mul(f32x4{});
 #pragma unroll
-               for (int i = 0; i < 4; ++i)
-                 if (c[i] > 0.f) o[x][e][i] += sign ? -INFINITY : INFINITY;
-             });
-        }
+                 for (int i = 0; i < 4; ++i)
+                   if (c[i] > 0.f) o[x][e][i] += sign ? -INFINITY : INFINITY;
+               });
+          }
 #pragma unroll
-        for (int j = 0; j < SUB * 4; ++j)
+          for (int j = 0; j < SUB * 4; ++j)
 #pragma unroll
-          for (int n = 0; n < NB; ++n)
+            for (int n = 0; n < NB; ++n)
 #pragma unroll
-            for (int w = 0; w < VB / 4; ++w) {
-              uint32_t& v = vf[j][n].w[w];
-              if (kBf16) {
-                if ((v & 0x7f80u) == 0x7f80u) v &= 0xffff0000u;
-                if ((v & 0x7f800000u) == 0x7f800000u) v &= 0xffffu;
-              } else if ((v & 0x7f800000u) == 0x7f800000u) {
-                v = 0;
+              for (int w = 0; w < VB / 4; ++w) {
+                uint32_t& v = vf[j][n].w[w];
+                if (kBf16) {
+                  if ((v & 0x7f80u) == 0x7f80u) v &= 0xffff0000u;
+                  if ((v & 0x7f800000u) == 0x7f800000u) v &= 0xffffu;
+                } else if ((v & 0x7f800000u) == 0x7f800000u) {
+                  v = 0;
+                }
               }
-            }
+        }
       }
       pv([&](int j, int n, int w) { return vf[j][n].w[w]; }, [&](int x, int j) { return p[x][j]; },
          [&](int x, int e, auto mul) { o[x][e] = mul(o[x][e]); });
       load_v();
-    };
-    // tiles whose keys every row sees, then those with the step's own rows
-    const int t_full = min(t_end, min(q.cached, q.len) / KT);
-    for (; tile < t_full; tile += kWaves) step(std::false_type{});
-    for (; tile < t_end; tile += kWaves) step(std::true_type{});
+    }
 
-    // The wavefronts' results, 16 query vectors at a time, merged through LDS:
-    // O = sum_w 2^(m_w - M) O_w.  A maximum of -inf has weight 0; where all are
-    // -inf the sum is 0 (no key seen) or NaN (only scores of -inf seen).
-    const int slot = 2 * blockIdx.x + (first_seg ? 0 : 1);
+    // The wavefronts' results, 16 query vectors at a time, merged through LDS.
+    const int64_t slot = 2 * (int64_t)blockIdx.x + (first_seg ? 0 : 1);
 #pragma unroll
     for (int x = 0; x < NR; ++x) {
       float lt = group_sum(l[x]);
-      if (seen[x] && m[x] == -INFINITY) lt = __builtin_nanf("");
-      __syncthreads();  // the previous 16 have been read
+      if (seen[x] && m[x] == -INFINITY) lt = __builtin_nanf("");  // only scores of -inf were seen
+      if (x > 0 || !first_seg) __syncthreads();  // the previous 16 have been read
       if (lg == 0) {
         s_m[wave][ln] = m[x];
         s_l[wave][ln] = lt;
       }
+      float* to = s_o + (wave * 16 + ln) * kPad + VW * 4 * lg;
 #pragma unroll
       for (int n = 0; n < NB; ++n)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float* d = s_o + (wave * 16 + ln) * kPad + n * 16 * VW + VW * (4 * lg + i);
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int e = 0; e < VW; ++e) d[e] = o[x][n * VW + e][i];
-        }
+          for (int e = 0; e < VW; ++e) to[n * 16 * VW + VW * i + e] = o[x][n * VW + e][i];
       __syncthreads();
+      const SplitArgs A = args();
       const int r = tid >> 4, c = tid & 15;  // 16 threads a query vector, D / 16 elements each
       const int qv = rt * RT + 16 * x + r;
-      if (qv < q.n * t.G) {
-        float M = -INFINITY, sum = 0.f, wgt[kWaves], acc[D / 16];
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_m[w][r]);
+      if (qv < q.n * A.t.G) {
+        constexpr int C = D / 16;
+        float2 ml[kWaves];
+        float v[kWaves][C];
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-          wgt[w] = s_m[w][r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[w][r] - M);
-          sum += s_m[w][r] == -INFINITY ? (M == -INFINITY ? s_l[w][r] : 0.f) : wgt[w] * s_l[w][r];
+          ml[w] = make_float2(s_m[w][r], s_l[w][r]);
+#pragma unroll
+          for (int e = 0; e < C; ++e) v[w][e] = s_o[(w * 16 + r) * kPad + c * C + e];
         }
-#pragma unroll
-        for (int e = 0; e < D / 16; ++e) acc[e] = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w)
-          if (wgt[w] != 0.f)
-#pragma unroll
-            for (int e = 0; e < D / 16; ++e) acc[e] = fmaf(wgt[w], s_o[(w * 16 + r) * kPad + c * (D / 16) + e], acc[e]);
-        const int i = a.group.div(qv), head = h * t.G + qv - i * t.G;
-        if (whole) {
-          const float inv = sum == 0.f && M == -INFINITY ? 0.f : 1.f / sum;
-          E* op = (E*)t.out + (q.r0 + i) * t.o_row + head * t.o_head + c * (D / 16);
+        Merge<C> mg;
+        mg.add(ml, v);
+        if (seg == ntile) {
+          const int i = A.group.div(qv), head = h * A.t.G + qv - i * A.t.G;
+          const float by = mg.scale();
+          E* op = (E*)A.t.out + (int64_t)(q.r0 + i) * A.t.o_row + head * A.t.o_head + c * C;
           if constexpr (kBf16) {
 #pragma unroll
-            for (int e = 0; e < D / 16; e += 2) *(uint32_t*)(op + e) = pack_bf16x2(acc[e] * inv, acc[e + 1] * inv);
+            for (int e = 0; e < C; e += 2) *(uint32_t*)(op + e) = pack_bf16x2(mg.acc[e] * by, mg.acc[e + 1] * by);
           } else {
 #pragma unroll
-            for (int e = 0; e < D / 16; ++e) op[e] = acc[e] * inv;
+            for (int e = 0; e < C; ++e) op[e] = mg.acc[e] * by;
           }
-          if (t.lse && c == 0) t.lse[(int64_t)(q.r0 + i) * t.Hq + head] = (M + __log2f(sum)) * kLn2;
+          if (A.t.lse && c == 0) A.t.lse[(int64_t)(q.r0 + i) * A.t.Hq + head] = mg.lse();
         } else {
-          float* pp = a.part + ((int64_t)slot * RT + 16 * x + r) * D + c * (D / 16);
+          const int64_t pr = slot * RT + 16 * x + r;
+          float* pp = A.part + pr * D + c * C;
 #pragma unroll
-          for (int e = 0; e < D / 16; ++e) pp[e] = acc[e];
-          if (c == 0) {
-            float* ml = a.part_ml + ((int64_t)slot * RT + 16 * x + r) * 2;
-            ml[0] = M;
-            ml[1] = sum;
-          }
+          for (int e = 0; e < C; ++e) pp[e] = mg.acc[e];
+          if (c == 0) *(float2*)(A.part_ml + pr * 2) = make_float2(mg.m, mg.sum);
         }
       }
     }
