@@ -164,7 +164,7 @@ __device__ __forceinline__ float group_sum(float x) {
 }
 
 template <typename E, int D, int NR>
-__global__ __launch_bounds__(kThreads, NR * D * sizeof(E) <= 256 ? 2 : 1) void tree_attend(const SplitArgs) {
+__global__ __launch_bounds__(kThreads, 2) void tree_attend(const SplitArgs) {
   constexpr bool kBf16 = sizeof(E) == 2;
   constexpr int SUB = kBf16 ? 2 : 1;             // 16-key pieces of a tile
   constexpr int KT = 16 * SUB;
@@ -665,7 +665,7 @@ static int row_groups(const Geo& g, const cs_batch& b) {
   const int64_t rows = b.max_rows > 0 ? b.max_rows : b.n_rows;
   const int64_t qv = rows * g.G;
   if (qv <= (wide_type(g) ? 32 : 16) || g.D > 128) return 1;
-  return qv <= 256 || g.D * g.esize >= 256 ? 2 : 4;
+  return qv <= 256 || g.D * g.esize > 128 ? 2 : 4;
 }
 
 // Whether the kernel for many rows takes the batch (where its pointers are
@@ -696,7 +696,7 @@ static void run_split(const SplitArgs& a, hipStream_t s) {
 }
 template <typename E, int D>
 static void run_split(const SplitArgs& a, int nr, hipStream_t s) {
-  if constexpr (D * sizeof(E) < 256)
+  if constexpr (D * sizeof(E) <= 128)
     if (nr == 4) return run_split<E, D, 4>(a, s);
   if constexpr (D <= 128)
     if (nr == 2) return run_split<E, D, 2>(a, s);
