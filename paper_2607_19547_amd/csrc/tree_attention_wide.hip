@@ -207,8 +207,7 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
     float m_use = -INFINITY, l_run = 0.f;
     bool seen = false;
 
-    auto qk = [&](auto B, f32x16& s0, f32x16& s1) {
-      const char* K = kbuf(B);
+    auto qk = [&](const char* K, f32x16& s0, f32x16& s1) {
       s0 = f32x16{};
       s1 = f32x16{};
 #pragma unroll
@@ -274,8 +273,7 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
     // of -inf (or NaN) that its row sees; those give it the infinity, both of
     // them NaN.  Then the values become zero in LDS.  (After the accumulators
     // are rescaled for the tile: their first factor is 0.)
-    auto not_finite = [&](auto C, int kt) {
-      char* V = vbuf(C);
+    auto not_finite = [&](char* V, int kt) {
       uint32_t odd = 0;
       for (int x = lane; x < kKT * kRow / 16; x += 64) {
         const u32x4 v = *(const u32x4*)(V + 16 * x);
@@ -344,8 +342,7 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
         m_use = m_new;
       }
     };
-    auto qk_head = [&](auto N, f32x16& n0, f32x16& n1) {
-      const char* K = kbuf(N);
+    auto qk_head = [&](const char* K, f32x16& n0, f32x16& n1) {
       n0 = f32x16{};
       n1 = f32x16{};
 #pragma unroll
@@ -358,9 +355,7 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
     };
     // Probabilities of the current tile, O^T += V^T P^T, and k-steps 2..7 of
     // the next tile's S^T in one straight-line block.
-    auto exp_pv_qk = [&](auto C, auto N, f32x16& s0, f32x16& s1, f32x16& n0, f32x16& n1) {
-      const char* V = vbuf(C);
-      const char* K = kbuf(N);
+    auto exp_pv_qk = [&](const char* V, const char* K, f32x16& s0, f32x16& s1, f32x16& n0, f32x16& n1) {
       __builtin_amdgcn_iglp_opt(3);
       const float nm = m_use == -INFINITY ? 0.f : -m_use;
       bf16x8 pb[4];
@@ -393,33 +388,64 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
     // Tile i is in ring slot C, tile i + 1 in N; tile i + 3 goes to S (read last
     // in step i - 1).  Each wavefront waits for its part of tile i + 2 (all but
     // its four newest loads) before the barrier.
-    const int t_clear = bad ? 0 : min(q.cached, q.len) / kKT - t0;  // tiles before it need no mask
     auto step = [&](auto C, auto N, auto S, int i, f32x16& c0, f32x16& c1, f32x16& n0, f32x16& n1) {
-      const int kt = key_begin + i * kKT;
       fetch(i + 3, kbuf(S), vbuf(S));
-      if (i >= t_clear) mask(kt, c0, c1);
-      else seen = true;
-      if (kt <= w_seen) {
-        qk_head(N, n0, n1);
+      if (w_seen >= 0) {
+        qk_head(kbuf(N), n0, n1);
         tile_max(c0, c1);
+        exp_pv_qk(vbuf(C), kbuf(N), c0, c1, n0, n1);
       }
-      if (i >= t_clear) not_finite(C, kt);  // (has barriers: every wavefront)
-      if (kt <= w_seen) exp_pv_qk(C, N, c0, c1, n0, n1);
       asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
       __builtin_amdgcn_s_barrier();
     };
+    // First the tiles that every row sees whole, their ring slots known to the
+    // compiler, a tile's scores computed a step ahead; then, in a plain loop, the
+    // few with the step's own rows.
+    const int n_clear = bad ? 0 : min(max(min(q.cached, q.len) / kKT - t0, 0), n_kt);
     f32x16 sa0, sa1, sb0, sb1;
     asm volatile("s_waitcnt vmcnt(4)" ::: "memory");  // tiles 0 and 1 and the queries have landed
     __builtin_amdgcn_s_barrier();
-    qk(I0{}, sa0, sa1);
-    for (int i = 0; i < n_kt; i += 4) {
+    if (n_clear > 0) qk(up_k0, sa0, sa1);
+    for (int i = 0; i < n_clear; i += 4) {
       step(I0{}, I1{}, I3{}, i, sa0, sa1, sb0, sb1);
-      if (i + 1 >= n_kt) break;
+      if (i + 1 >= n_clear) break;
       step(I1{}, I2{}, I0{}, i + 1, sb0, sb1, sa0, sa1);
-      if (i + 2 >= n_kt) break;
+      if (i + 2 >= n_clear) break;
       step(I2{}, I3{}, I1{}, i + 2, sa0, sa1, sb0, sb1);
-      if (i + 3 >= n_kt) break;
+      if (i + 3 >= n_clear) break;
       step(I3{}, I0{}, I2{}, i + 3, sb0, sb1, sa0, sa1);
+    }
+    seen = n_clear > 0;
+    auto k_at = [&](int x) -> char* { return x & 2 ? (x & 1 ? up_k3 : up_k2) : (x & 1 ? up_k1 : up_k0); };
+    auto v_at = [&](int x) -> char* { return x & 2 ? (x & 1 ? lo_v3 : lo_v2) : (x & 1 ? lo_v1 : lo_v0); };
+#pragma unroll 1
+    for (int i = n_clear; i < n_kt; ++i) {
+      const int kt = key_begin + i * kKT;
+      fetch(i + 3, k_at(i + 3), v_at(i + 3));
+      char* V = v_at(i);
+      if (kt <= w_seen) {
+        qk(k_at(i), sa0, sa1);
+        mask(kt, sa0, sa1);
+        tile_max(sa0, sa1);
+      }
+      not_finite(V, kt);  // (has barriers: every wavefront)
+      if (kt <= w_seen) {
+        const float nm = m_use == -INFINITY ? 0.f : -m_use;
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+          bf16x8 pb;
+#pragma unroll
+          for (int x = 0; x < 8; ++x) {
+            const float p = __builtin_amdgcn_exp2f(fmaf((ks < 2 ? sa0 : sa1)[8 * (ks & 1) + x], sc, nm));
+            l_run += p;
+            pb[x] = (__bf16)p;
+          }
+#pragma unroll
+          for (int d = 0; d < 4; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(V, ks, d), pb, o[d], 0, 0, 0);
+        }
+      }
+      asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 
