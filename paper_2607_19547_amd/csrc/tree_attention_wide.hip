@@ -145,19 +145,7 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
       const int qv = min(v0 + ql, vectors - 1);
       g_row = A.group.div(qv);
       w_seen = v0 >= vectors ? -1 : A.t.mask ? q.len : q.cached + uniform(A.group.div(min(v0 + 31, vectors - 1)));
-      const uint16_t* qp = (const uint16_t*)A.t.q + (int64_t)(q.r0 + g_row) * A.t.q_row +
-                           (h * A.t.G + qv - g_row * A.t.G) * A.t.q_head + 8 * hi;
-#pragma unroll
-      for (int s = 0; s < 8; ++s) qb[s] = *(const bf16x8*)(qp + 16 * s);
-      // pages of this piece that are none of the pool
-      bad = 0;
-      if (n_kt > 0) {
-        const int p0 = A.t.page.div(key_begin), p1 = A.t.page.div(min(key_begin + n_kt * kKT, q.len) - 1);
-        const int32_t* tb = A.t.table + (int64_t)b * A.t.max_blocks;
-        for (int x = p0 + tid; x <= p1; x += kWideThreads) bad |= tb[x] < 0 || tb[x] >= A.t.pool.n_pages;
-      }
     }
-    bad = __syncthreads_or(bad);  // (the ring is free as well: every wavefront has left the previous piece)
 
     // this wavefront's 8 keys of tile i: their page, and the loads into a ring
     // slot (what they need of the arguments stays in scalar registers: read
@@ -199,7 +187,23 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
     find_page(0);
     fetch(0, up_k0, lo_v0);
     fetch(1, up_k1, lo_v1);
+    {
+      const SplitArgs A = args();
+      const int qv = min(rt * 256 + 32 * wave + ql, q.n * A.t.G - 1);
+      const uint16_t* qp = (const uint16_t*)A.t.q + (int64_t)(q.r0 + g_row) * A.t.q_row +
+                           (h * A.t.G + qv - g_row * A.t.G) * A.t.q_head + 8 * hi;
+#pragma unroll
+      for (int s = 0; s < 8; ++s) qb[s] = *(const bf16x8*)(qp + 16 * s);
+      // pages of this piece that are none of the pool
+      bad = 0;
+      if (n_kt > 0) {
+        const int p0 = A.t.page.div(key_begin), p1 = A.t.page.div(min(key_begin + n_kt * kKT, q.len) - 1);
+        const int32_t* tb = A.t.table + (int64_t)b * A.t.max_blocks;
+        for (int x = p0 + tid; x <= p1; x += kWideThreads) bad |= tb[x] < 0 || tb[x] >= A.t.pool.n_pages;
+      }
+    }
     fetch(2, up_k2, lo_v2);
+    bad = __syncthreads_or(bad);
 
     f32x16 o[4];
 #pragma unroll
