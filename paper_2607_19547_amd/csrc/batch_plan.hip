@@ -15,10 +15,11 @@ namespace cs {
 // The arrays are small (a few KB to a MB) and the step waits for them, so the
 // launch is bound by its latency: one launch, in which every workgroup makes
 // both prefix sums for itself (the lengths come from the L2) and then writes
-// its own 256 rows and its own share of the requests.  Nothing passes between
-// workgroups, since no array is read that the launch writes: a row's page is
-// the table's where the request held it before, the free list's otherwise.
+// its own 256 rows or its own 64 requests.  Nothing passes between workgroups,
+// since no array is read that the launch writes: a row's page is the table's
+// where the request held it before, the free list's otherwise.
 constexpr int kPlanThreads = 256;
+constexpr int kPlanRequests = 64;    // requests of a workgroup
 constexpr int kParentWindow = 2048;  // parents kept in LDS: the workgroup's rows and the tree before them
 
 struct BatchPlanArgs {
@@ -38,102 +39,106 @@ struct BatchPlanArgs {
   int32_t* free_head_out;
   int32_t* status;
   int B, n_rows, max_blocks, words, n_free, n_pages;
+  unsigned row_blocks;  // workgroups for rows; the others take requests
   FastDiv page;
 };
 
-// Sums of x over the workgroup's threads before this one; *total gets the sum.
-__device__ __forceinline__ int64_t block_scan64(int64_t x, int64_t* red, int64_t* total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t inc = wave_scan64(x);
-  if (lane == 63) red[wave] = inc;
-  __syncthreads();
-  int64_t before = 0, sum = 0;
-  for (int w = 0; w < kPlanThreads / 64; ++w) {
-    before += w < wave ? red[w] : 0;
-    sum += red[w];
-  }
-  __syncthreads();  // red is used again
-  *total = sum;
-  return before + inc - x;
+// Prefix sums over the wavefront that stay at 2^32 - 1 once they get there, so
+// that a sum beyond the arrays' sizes is seen as one.
+__device__ __forceinline__ unsigned wave_scan_sat(unsigned x) {
+  auto add = [](unsigned u, int v) { return __builtin_elementwise_add_sat(u, (unsigned)v); };
+  x = add(x, __builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false));  // row_shr 1, 2, 4, 8
+  x = add(x, __builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false));
+  x = add(x, __builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false));
+  x = add(x, __builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false));
+  x = add(x, __builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false));  // lane 15 to rows 1 and 3
+  x = add(x, __builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false));  // lane 31 to rows 2 and 3
+  return x;
 }
 
 __global__ __launch_bounds__(kPlanThreads) void batch_plan(const BatchPlanArgs a) {
   extern __shared__ int lds[];
   int* s_row = lds;                // [B + 1] first row of request b
-  int* s_take = lds + a.B + 1;     // [B] first entry of the free list that request b takes
-  int* s_par = s_take + a.B;       // [kParentWindow]
-  __shared__ int64_t red[kPlanThreads / 64];
-  __shared__ int s_flags;
-  const int tid = threadIdx.x, P = a.page.d;
-  if (tid == 0) s_flags = 0;
-  __syncthreads();
+  int* s_take = lds + a.B + 1;     // [B + 1] first entry of the free list that request b takes
+  int* s_par = s_take + a.B + 1;   // [kParentWindow]
+  __shared__ unsigned s_rows[kPlanThreads / 64], s_grow[kPlanThreads / 64];
+  __shared__ int s_flags[kPlanThreads / 64];
+  const int tid = threadIdx.x, P = a.page.d, lane = tid & 63, wave = tid >> 6;
   const int head = *a.free_head;
   // each thread takes `per` consecutive requests
   const int per = (a.B + kPlanThreads - 1) / kPlanThreads;
-  int64_t rows = 0, grow = 0;
+  const int b0 = min(tid * per, a.B), b1 = min(b0 + per, a.B);
+  unsigned rows = 0, grow = 0;
   int flags = head < 0 ? CS_PLAN_BAD_LENGTH : 0;
-  for (int j = 0; j < per; ++j) {
-    const int b = tid * per + j;
-    if (b >= a.B) break;
+  for (int b = b0; b < b1; ++b) {
     const int c = a.cached[b], n = a.new_len[b], h = a.held[b];
     if (c < 0 || n < 0 || h < 0 || (int64_t)c + n > 0x7fffffff || (int64_t)h * P < c) flags |= CS_PLAN_BAD_LENGTH;
     if (n > a.n_rows) flags |= CS_PLAN_TOO_MANY_ROWS;
     if (a.mask && n > 64 * (int64_t)a.words) flags |= CS_PLAN_MASK_TOO_SMALL;
-    const int64_t need = ((int64_t)c + n + P - 1) / P;
+    const int last = (int)min((unsigned)max(c, 0) + (unsigned)max(n, 0), 0x7fffffffu) - 1;
+    const int need = last < 0 ? 0 : a.page.div(last) + 1, more = max(need - max(h, 0), 0);
     if (need > a.max_blocks || h > a.max_blocks) flags |= CS_PLAN_TABLE_FULL;
-    rows += max(n, 0);
-    grow += max(need - h, (int64_t)0);
+    rows = __builtin_elementwise_add_sat(rows, (unsigned)max(n, 0));
+    grow = __builtin_elementwise_add_sat(grow, (unsigned)more);
+    s_row[b] = n;
+    s_take[b] = more;
   }
-  int64_t n_total, n_grow;
-  const int64_t row0 = block_scan64(rows, red, &n_total);
-  const int64_t take0 = block_scan64(grow, red, &n_grow);
-  if (n_total > a.n_rows) flags |= CS_PLAN_TOO_MANY_ROWS;
-  if (head + n_grow > a.n_free) flags |= CS_PLAN_POOL_FULL;
-  if (flags) atomicOr(&s_flags, flags);
+  const unsigned up_rows = wave_scan_sat(rows), up_grow = wave_scan_sat(grow);
+  if (__ballot(flags))
+    for (int o = 1; o < 64; o <<= 1) flags |= __shfl_xor(flags, o);
+  if (lane == 63) {
+    s_rows[wave] = up_rows;
+    s_grow[wave] = up_grow;
+    s_flags[wave] = flags;
+  }
   __syncthreads();
-  flags = s_flags;
-  const bool ok = flags == 0;
-  if (!ok) {
-    n_total = 0;
-    n_grow = 0;
+  unsigned n_total = 0, n_grow = 0, row0 = up_rows - rows, take0 = up_grow - grow;
+#pragma unroll
+  for (int w = 0; w < kPlanThreads / 64; ++w) {
+    row0 += w < wave ? s_rows[w] : 0;
+    take0 += w < wave ? s_grow[w] : 0;
+    n_total = __builtin_elementwise_add_sat(n_total, s_rows[w]);
+    n_grow = __builtin_elementwise_add_sat(n_grow, s_grow[w]);
+    flags |= s_flags[w];
   }
-  {
-    int r = ok ? (int)row0 : 0, t = head + (ok ? (int)take0 : 0);
-    for (int j = 0; j < per; ++j) {
-      const int b = tid * per + j;
-      if (b >= a.B) break;
-      s_row[b] = r;
-      s_take[b] = t;
-      if (ok) {
-        const int n = a.new_len[b];
-        r += n;
-        t += max((int)(((int64_t)a.cached[b] + n + P - 1) / P) - a.held[b], 0);
-      }
-    }
-    if (tid == 0) s_row[a.B] = (int)n_total;
+  if (n_total > (unsigned)a.n_rows) flags |= CS_PLAN_TOO_MANY_ROWS;
+  if ((int64_t)head + n_grow > a.n_free) flags |= CS_PLAN_POOL_FULL;
+  const bool ok = flags == 0;
+  if (!ok) n_total = n_grow = row0 = take0 = 0;
+  take0 += head;
+  for (int b = b0; b < b1; ++b) {
+    const int n = s_row[b], more = s_take[b];
+    s_row[b] = row0;
+    s_take[b] = take0;
+    row0 += ok ? n : 0;
+    take0 += ok ? more : 0;
+  }
+  if (tid == 0) {
+    s_row[a.B] = n_total;
+    s_take[a.B] = head + n_grow;
   }
   __syncthreads();
 
-  // the workgroup's share of the requests: what the step leaves of them
-  const int share = (a.B + gridDim.x - 1) / gridDim.x;
-  const int b_end = min((int)(blockIdx.x + 1) * share, a.B);
-  for (int b = blockIdx.x * share + (tid >> 4); b < b_end; b += kPlanThreads / 16) {  // 16 threads a request
-    const int h = a.held[b];
-    const int need = ok ? (int)(((int64_t)a.cached[b] + a.new_len[b] + P - 1) / P) : h;
-    for (int x = h + (tid & 15); x < need; x += 16) {
-      const int page = a.free_pages[s_take[b] + x - h];
-      a.table[(int64_t)b * a.max_blocks + x] = page;
-      if (page < 0 || page >= a.n_pages) atomicOr(a.status, CS_PLAN_BAD_PAGE);
+  if (blockIdx.x >= a.row_blocks) {  // requests: what the step leaves of them
+    const int first = (blockIdx.x - a.row_blocks) * kPlanRequests;
+    for (int b = first + (tid >> 2); b < min(first + kPlanRequests, a.B); b += kPlanThreads / 4) {  // 4 threads each
+      const int h = a.held[b], take = s_take[b], more = s_take[b + 1] - take;
+      for (int x = tid & 3; x < more; x += 4) {
+        const int page = a.free_pages[take + x];
+        a.table[(int64_t)b * a.max_blocks + h + x] = page;
+        if (page < 0 || page >= a.n_pages) atomicOr(a.status, CS_PLAN_BAD_PAGE);
+      }
+      if ((tid & 3) == 0) {
+        a.held_out[b] = h + more;
+        a.row_start[b] = s_row[b];
+      }
     }
-    if ((tid & 15) == 0) {
-      a.held_out[b] = max(need, h);
-      a.row_start[b] = s_row[b];
+    if (first == 0 && tid == 0) {
+      a.row_start[a.B] = n_total;
+      *a.free_head_out = head + n_grow;
+      if (flags) atomicOr(a.status, flags);
     }
-  }
-  if (blockIdx.x == 0 && tid == 0) {
-    a.row_start[a.B] = (int)n_total;
-    *a.free_head_out = head + (int)n_grow;
-    if (flags) atomicOr(a.status, flags);
+    return;
   }
 
   // the workgroup's rows
@@ -149,14 +154,14 @@ __global__ __launch_bounds__(kPlanThreads) void batch_plan(const BatchPlanArgs a
     return lo;
   };
   int w0 = 0, w1 = 0;  // rows whose parents are in LDS
-  if (a.parent && r_first < n_total) {
+  if (a.parent && r_first < (int)n_total) {
     w1 = min(r_first + kPlanThreads, (int)n_total);
     w0 = max(s_row[request_at(r_first)], w1 - kParentWindow);
     for (int x = w0 + tid; x < w1; x += kPlanThreads) s_par[x - w0] = a.parent[x];
     __syncthreads();
   }
   if (r >= a.n_rows) return;
-  if (r >= n_total) {
+  if (r >= (int)n_total) {
     a.slot[r] = -1;
     return;
   }
@@ -206,7 +211,8 @@ __global__ __launch_bounds__(kPlanThreads) void batch_plan(const BatchPlanArgs a
 
 cs_status launch_batch_plan(const Geo& g, int64_t n_pages, const cs_batch& b, const cs_page_plan& p, hipStream_t s,
                             bool check_only) {
-  const int64_t blocks = std::max<int64_t>(1, ((int64_t)b.n_rows + kPlanThreads - 1) / kPlanThreads);
+  const int64_t row_blocks = ((int64_t)b.n_rows + kPlanThreads - 1) / kPlanThreads;
+  const int64_t blocks = row_blocks + std::max(1, (b.n_requests + kPlanRequests - 1) / kPlanRequests);
   const cs_status st = check_grid(blocks, 1, 1, kPlanThreads, "batch plan");
   if (st || check_only) return st;
   BatchPlanArgs a;
@@ -232,8 +238,9 @@ cs_status launch_batch_plan(const Geo& g, int64_t n_pages, const cs_batch& b, co
   a.n_free = p.n_free;
   a.n_pages = (int)n_pages;
   a.page = fast_div((int)g.T);
+  a.row_blocks = (unsigned)row_blocks;
   TraceScope tr("batch_plan", s);
-  const size_t lds = (2 * (size_t)a.B + 1 + (p.parent ? kParentWindow : 0)) * sizeof(int);
+  const size_t lds = (2 * (size_t)a.B + 2 + (p.parent ? kParentWindow : 0)) * sizeof(int);
   CS_LAUNCH(tr, batch_plan, dim3((unsigned)blocks), dim3(kPlanThreads), lds, s, a);
   return check_launch("batch plan launch");
 }
