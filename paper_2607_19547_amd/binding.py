@@ -171,14 +171,14 @@ def _stream(stream):
     """The address of the stream given, or of torch's current one (looked up without making a
     Stream object where torch has that call: 0.3 us instead of 3)."""
     if stream is not None:
-        return ctypes.c_void_p(stream)
+        return stream
     global _raw_stream
     import torch
     if _raw_stream is None:
         torch.cuda.current_stream()  # (initialises the runtime, and says why where it cannot)
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
             lambda device: torch.cuda.current_stream(device).cuda_stream)
-    return ctypes.c_void_p(_raw_stream(torch.cuda.current_device()))
+    return _raw_stream(torch.cuda.current_device())
 
 
 def compose_rebase_k(geo, k_cache, chunk_offsets, local_coords=None, want_global=False, stream=None):

@@ -657,15 +657,20 @@ static bool has_instance(const Geo& g) {
 }
 static bool wide_type(const Geo& g) { return g.dtype == CS_BF16 && g.D == 128; }
 // Row tiles of 16, 32 or 64 query vectors.  A larger one reads the keys fewer
-// times and leaves fewer wavefronts to a SIMD; with rows of 256 bytes and more
-// 64 do not fit the registers.  Measured (us): 65,000 tokens, 8 query heads a KV
-// head, float32 x 128, 17 rows: 169 / 114 / 388 with 16 / 32 / 64; bf16 x 64, 64
-// rows: 93 / 79 / 66, but 4 requests of up to 4,096 tokens, 17 rows: 14 / 14 / 19.
+// times, in fewer and longer pieces of work; with rows of more than 128 bytes 64
+// do not fit the registers.  Row tiles of 16 win where they read little in all:
+// measured (us with 16 / 32, 8 query heads a KV head, 6 and 17 rows, 4,000 to
+// 32,000 tokens), the two meet near 200 MB for float32 x 128 (147 MB: 23 / 28, 295
+// MB: 47 / 38), 130 MB for float32 x 64 (74: 16 / 20, 295: 46 / 34) and 90 MB for
+// bf16 x 64 (37: 12 / 14, 147: 24 / 21).  The host knows only the block tables'
+// room, which is seldom filled: the border is put at 1.6 times that.
 static int row_groups(const Geo& g, const cs_batch& b) {
   const int64_t rows = b.max_rows > 0 ? b.max_rows : b.n_rows;
   const int64_t qv = rows * g.G;
   if (qv <= (wide_type(g) ? 32 : 16) || g.D > 128) return 1;
-  return qv <= 256 || g.D * g.esize > 128 ? 2 : 4;
+  const double row_bytes = g.D * g.esize, room = (double)b.n_requests * b.max_blocks * g.T * g.Hkv * row_bytes * 2;
+  if (room * ((qv + 15) / 16) < 1.6 * (50e6 + 0.3e6 * row_bytes)) return 1;
+  return qv <= 256 || row_bytes > 128 ? 2 : 4;
 }
 
 // Whether the kernel for many rows takes the batch (where its pointers are
