@@ -75,6 +75,13 @@ cs_status check_written(const Geo& g, const cs_rows* r, int n_rows, int heads, c
   return CS_OK;
 }
 
+// Rows x heads are counted in 32 bits.
+cs_status check_row_count(const Geo& g, const cs_batch& b) {
+  if ((int64_t)b.n_rows * (g.Hq + 2 * (int64_t)g.Hkv) >= (int64_t(1) << 31))
+    return fail(CS_ERR_UNSUPPORTED, "rows x heads must be below 2^31");
+  return CS_OK;
+}
+
 cs_status check_layer(const Geo& g, int32_t layer) {
   if (layer < 0 || layer >= g.L) return fail(CS_ERR_INVALID_ARGUMENT, "layer out of range");
   return CS_OK;
@@ -130,7 +137,8 @@ cs_status qk_norm_rope_append(const cs_geometry* page, const cs_page_pool* pool,
   if (!(eps >= 0.f && isfinite(eps))) return fail(CS_ERR_INVALID_ARGUMENT, "eps must be finite and >= 0");
   if (batch->n_requests == 0 || batch->n_rows == 0) return CS_OK;
   if (!batch->slot || !batch->coords) return fail(CS_ERR_INVALID_ARGUMENT, "slot or coords is NULL");
-  st = check_rows(q, "q");
+  st = check_row_count(g, *batch);
+  if (!st) st = check_rows(q, "q");
   if (!st) st = check_rows(k, "k");
   if (!st) st = check_rows(v, "v");
   if (!st) st = check_rows(q_out, "q_out");
@@ -165,7 +173,8 @@ cs_status tree_attend_paged(const cs_geometry* page, const cs_page_pool* pool, i
   if (!st) st = check_batch(batch);
   if (st) return st;
   if (batch->n_requests == 0 || batch->n_rows == 0) return CS_OK;
-  st = check_rows(q, "q");
+  st = check_row_count(g, *batch);
+  if (!st) st = check_rows(q, "q");
   if (!st) st = check_rows(out, "out");
   if (!st) st = check_written(g, out, batch->n_rows, g.Hq, "out");
   if (st) return st;

@@ -1,6 +1,10 @@
 // Shared by the sources of the batch attention: its arguments and how its work is cut.
 #pragma once
 
+#include <math.h>
+
+#include <algorithm>
+
 #include "batch.h"
 
 namespace cs {
@@ -113,7 +117,7 @@ __device__ __forceinline__ bool find_run(const SplitArgs& a, int w, Run* run) {
   int64_t off = begin - lane_value(upto - sum, at);
   int b = at * per;
   if (per > 1)  // (the whole wavefront walks, off the scalar cache)
-    for (;; ++b) {
+    for (; b < a.t.B - 1; ++b) {
       int nrt, ntile;
       unit_sizes(a, load_request_scalar(a.t, b), &nrt, &ntile);
       const int64_t x = (int64_t)a.t.Hkv * nrt * ntile;
@@ -169,6 +173,14 @@ struct Merge {
   __device__ __forceinline__ float scale() const { return m == -INFINITY && sum == 0.f ? 0.f : 1.f / sum; }
   __device__ __forceinline__ float lse() const { return (m + __log2f(sum)) * kLn2; }
 };
+
+// Workgroups that a launch needs at most: the runs there can be, from the rows
+// and the block tables' room.  A batch with room for one run needs no merge.
+inline int most_runs(const SplitArgs& a) {
+  const double tiles = std::max<double>(1, ((double)a.t.max_blocks * a.t.page.d + (1 << a.tile_bits) - 1) / (1 << a.tile_bits));
+  const double units = ((double)a.t.n_rows * a.t.G / (1 << a.row_bits) + a.t.B) * a.t.Hkv;
+  return (int)std::min<double>(1 << a.run_bits, ceil(tiles * units / a.min_tiles) + 1);
+}
 
 // The instance for many rows (bf16, head_dim 128): see tree_attention_wide.hip.
 constexpr int kWideRowBits = 8, kWideTileBits = 6, kWideRunBits = 8;

@@ -202,6 +202,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const SplitArgs) {
   while (left > 0) {
     const SplitArgs a = args();
     const TreeArgs& t = a.t;
+    if (b >= t.B) break;  // (lengths that changed meanwhile)
     const Request q = load_request_scalar(t, b);
     int nrt, ntile;
     unit_sizes(a, q, &nrt, &ntile);
@@ -692,12 +693,14 @@ size_t tree_attend_workspace(const Geo& g, const cs_batch& b) {
 
 template <typename E, int D, int NR>
 static void run_split(const SplitArgs& a, hipStream_t s) {
+  const int runs = most_runs(a);
   {
     TraceScope tr("tree_attend", s);
-    CS_LAUNCH(tr, (tree_attend<E, D, NR>), dim3(kRuns), dim3(kThreads), 0, s, a);
+    CS_LAUNCH(tr, (tree_attend<E, D, NR>), dim3(runs), dim3(kThreads), 0, s, a);
   }
+  if (runs == 1) return;
   TraceScope tr("tree_combine", s);
-  CS_LAUNCH(tr, (tree_combine<E, D>), dim3(kRuns - 1, 2 * NR), dim3(kThreads), 0, s, a);
+  CS_LAUNCH(tr, (tree_combine<E, D>), dim3(runs - 1, 2 * NR), dim3(kThreads), 0, s, a);
 }
 template <typename E, int D>
 static void run_split(const SplitArgs& a, int nr, hipStream_t s) {

@@ -119,6 +119,7 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
     int u, t0, nrt, ntile;
     {
       const SplitArgs A = args();
+      if (b >= A.t.B) break;  // (lengths that changed meanwhile)
       q = load_request_scalar(A.t, b);
       unit_sizes(A, q, &nrt, &ntile);
       if (off >= (int64_t)A.t.Hkv * nrt * ntile) {  // behind this request's units
@@ -600,12 +601,14 @@ void launch_tree_wide(SplitArgs a, void* ws, hipStream_t s) {
   a.min_tiles = 4;
   a.part = (float*)(((uintptr_t)ws + 255) & ~(uintptr_t)255);
   a.part_ml = a.part + 2 * (size_t)kWideRuns * kPartHalfs / 2;
+  const int runs = most_runs(a);
   {
     TraceScope tr("tree_attend_wide", s);
-    CS_LAUNCH(tr, tree_attend_wide, dim3(kWideRuns), dim3(kWideThreads), 0, s, a);
+    CS_LAUNCH(tr, tree_attend_wide, dim3(runs), dim3(kWideThreads), 0, s, a);
   }
+  if (runs == 1) return;
   TraceScope tr("tree_combine_wide", s);
-  CS_LAUNCH(tr, tree_combine_wide, dim3(kWideRuns - 1, kStripShare), dim3(kStripThreads), 0, s, a);
+  CS_LAUNCH(tr, tree_combine_wide, dim3(runs - 1, kStripShare), dim3(kStripThreads), 0, s, a);
 }
 
 }  // namespace cs

@@ -165,6 +165,12 @@ def test_attend_rows_and_workspace(built_lib):
         assert _attend(ws_bytes=n.value - 1) == SMALL and _attend(ws=None) == SMALL
 
 
+@pytest.mark.parametrize("call", [_append, _attend])
+def test_too_many_rows(built_lib, call):
+    assert call(batch=_batch(n_rows=1 << 29)) == UNS
+    _says("2^31")
+
+
 def test_commit_arguments(built_lib):
     assert _commit(lb=1, le=0) == BAD and _commit(lb=-1) == BAD and _commit(le=3) == BAD
     assert _commit(most=-1) == BAD and _commit(accepted=None) == BAD and _commit(count=None) == BAD
