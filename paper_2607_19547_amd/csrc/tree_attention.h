@@ -55,6 +55,8 @@ struct SplitArgs {
   FastDiv group;    // division by G
 };
 
+constexpr int kNonTemporal = 2;  // the buffer loads' cache policy bit
+
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ int64_t lane_value(int64_t x, int lane) {
   return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32) |
@@ -185,6 +187,10 @@ inline int most_runs(const SplitArgs& a) {
 // The instance for many rows (bf16, head_dim 128): see tree_attention_wide.hip.
 constexpr int kWideRowBits = 8, kWideTileBits = 6, kWideRunBits = 8;
 size_t tree_wide_workspace();
-void launch_tree_wide(SplitArgs a, void* ws, hipStream_t s);
+// once: keys and values with the non-temporal hint.  One row tile a request: 32 requests
+// of 8,000 tokens, 8 rows 72 -> 64 us; two and more read them again (tree-sized steps
+// of 65,000 tokens 59 -> 62).
+constexpr double kWideOnceBytes = 64e6;
+void launch_tree_wide(SplitArgs a, void* ws, bool once, hipStream_t s);
 
 }  // namespace cs

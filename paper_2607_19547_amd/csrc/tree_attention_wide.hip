@@ -51,6 +51,7 @@ __device__ __forceinline__ float pair_sum(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+template <bool ONCE>
 __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs a0) {
   // LDS rows are 256 bytes, a key each, their 16-byte chunks permuted so that
   // the operand reads are free of bank conflicts (K: chunk c of row r at c ^
@@ -180,8 +181,8 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const int r0 = 8 * wave + 4 * j;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void*)(Kd + r0 * kRow), 16, soff_k[j], 0, 0, 0);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void*)(Vd + r0 * kRow), 16, soff_v[j], 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void*)(Kd + r0 * kRow), 16, soff_k[j], 0, 0, ONCE ? kNonTemporal : 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void*)(Vd + r0 * kRow), 16, soff_v[j], 0, 0, ONCE ? kNonTemporal : 0);
       }
       find_page(i + 1);
     };
@@ -594,7 +595,7 @@ __global__ __launch_bounds__(kStripThreads) void tree_combine_wide(const SplitAr
 
 size_t tree_wide_workspace() { return 2 * (size_t)kWideRuns * (kPartHalfs * sizeof(_Float16) + 4 * 256 * sizeof(float)) + 512; }
 
-void launch_tree_wide(SplitArgs a, void* ws, hipStream_t s) {
+void launch_tree_wide(SplitArgs a, void* ws, bool once, hipStream_t s) {
   a.row_bits = kWideRowBits;
   a.tile_bits = kWideTileBits;
   a.run_bits = kWideRunBits;
@@ -604,7 +605,8 @@ void launch_tree_wide(SplitArgs a, void* ws, hipStream_t s) {
   const int runs = most_runs(a);
   {
     TraceScope tr("tree_attend_wide", s);
-    CS_LAUNCH(tr, tree_attend_wide, dim3(runs), dim3(kWideThreads), 0, s, a);
+    if (once) CS_LAUNCH(tr, tree_attend_wide<true>, dim3(runs), dim3(kWideThreads), 0, s, a);
+    else CS_LAUNCH(tr, tree_attend_wide<false>, dim3(runs), dim3(kWideThreads), 0, s, a);
   }
   if (runs == 1) return;
   TraceScope tr("tree_combine_wide", s);
