@@ -404,6 +404,10 @@ cs_status selective_attend_scatter_rope_paged(const cs_geometry* g, void* const*
  *     tree_attend_paged      per layer: attention of the rows
  *     tree_commit_paged      the rows of an accepted path become cached tokens
  *
+ * Requests may share pages that none of them writes: those that are full of
+ * cached tokens.  A request writes the page that its last cached token does not
+ * fill, and the ones behind it.
+ *
  * All the arrays of cs_batch are DEVICE memory, dense, and are read when the
  * stream gets there, so a captured graph can be replayed with new lengths.
  * Their contents cannot be checked by the host.  Whatever they hold, no call
@@ -498,13 +502,13 @@ cs_status batch_plan_pages(const cs_geometry* page, int64_t n_pages, const cs_ba
  * Eq. 2 at the row's coordinates, and the rows' keys and values put into their
  * pages, in one pass over the rows.
  *
- *   y = x / sqrt(mean_d x_d^2 + eps) * weight      (norm, per head)
+ *   y = x / sqrt(mean_d x_d^2 + eps) * weight      (norm, per head; the squares are float32)
  *   (y_i, y_{i+D/2}) turned by coords[axis(i)] * theta_i   (as everywhere here)
  * Queries go to q_out, keys and (unchanged) values to slot[r] of the pool in
  * `layer`.  Everything between is float32 (the angles float64), rounded once.
  * Rows whose slot is outside the pool write no key and no value; a row's query
  * is written whatever its slot is, for the rows below row_start[B] alone.
- * A slot that two rows share gets one of them.
+ * Two rows with one slot leave a mixture of both there.
  *
  *   q, k, v            [n_rows][H_q | H_kv | H_kv][D]
  *   q_weight, k_weight DEVICE [D], geometry.dtype, or NULL: that side is

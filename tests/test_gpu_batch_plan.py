@@ -104,6 +104,11 @@ def test_plan_writes_chain_masks_without_parents():
     assert np.array_equal(s.mask.cpu().numpy(), ob.mask_words(ref["mask"], 3))
 
 
+def test_plan_of_no_rows():
+    s = Step(16, [5, 0], [0, 0], [1, 0], [[4], [-1]], [3], 0, 0).run()
+    assert s.row_start.tolist() == [0, 0, 0] and s.held_out.tolist() == [1, 0] and s.status.item() == 0
+
+
 def test_plan_of_no_requests():
     s = Step(16, [], [], [], np.zeros((0, 4)), [3], 0, 4).run()
     assert s.row_start.tolist() == [0] and s.slot.tolist() == [-1] * 4 and s.head_out.item() == 0

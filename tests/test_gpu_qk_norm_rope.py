@@ -105,6 +105,12 @@ def test_without_norm_and_large_rows():
     Case(4, 700, 4, 4, 128, "f32", page=48, far=(1 << 31) - 1).check()  # coordinates up to the largest
 
 
+def test_room_for_many_rows():
+    """Row arrays with much room: another way of loading, the rows of the step alone."""
+    Case(9, 5, 16, 2, 128, "bf16", page=64, pad=13_500).check()
+    Case(10, 3, 4, 4, 128, "f32", page=64, pad=11_000).check()
+
+
 def test_in_place_queries_and_one_side_normed():
     c = Case(5, 21, 16, 2, 128, "bf16")
     c.w[1] = None

@@ -147,6 +147,13 @@ def test_strides_in_place_and_no_lse(geo):
     wide = torch.full((c.n_rows, c.hq + 3, c.d), 5.0, dtype=want.dtype, device="cuda")
     out, _ = _run(c, parts=parts, q=heads, out=wide[:, 1:1 + c.hq], lse=False)
     assert torch.equal(out, want) and (wide[:, 0] == 5).all() and (wide[:, -2:] == 5).all()
+    two = torch.full((c.n_rows, c.hq * c.d + 2), 5.0, dtype=want.dtype, device="cuda")  # out aligned to two elements
+    out, lse = _run(c, parts=parts, out=two[:, 2:].unflatten(1, (c.hq, c.d)))
+    check_attend(c, 1, out, lse, "out aligned to two elements")
+    assert (two[:, :2] == 5).all()
+    own = parts[3].clone()
+    out, _ = _run(c, parts=parts, q=own, out=own)  # in place, aligned
+    assert torch.equal(out, want)
     odd = torch.zeros(c.n_rows, c.hq * c.d + 1, dtype=want.dtype, device="cuda")  # nothing aligned
     q = odd[:, 1:].unflatten(1, (c.hq, c.d))
     q.copy_(parts[3])
@@ -159,6 +166,19 @@ def test_max_rows_is_a_hint(max_rows):
     """Any hint gives the results, for a batch of one-row and many-row requests."""
     _check(Case(8, [500, 70, 1500], [1, 90, 2], 64, 16, 2, 128), max_rows=max_rows)
     _check(Case(8, [500, 70], [1, 40], 48, 4, 2, 64, "f32"), max_rows=max_rows)
+
+
+@pytest.mark.parametrize("geo", [GEOS[0], GEOS[2], GEOS[5]])
+@pytest.mark.parametrize("new", [[1, 1], [1, 30]])
+def test_block_tables_with_much_room(geo, new):
+    """The room chooses how keys are fetched and how rows are tiled; the rest of a table is not read."""
+    _check(Case(14, [700, 90], new, 64, *geo, pad_blocks=2000))
+
+
+def test_short_batches_of_one_piece():
+    for cached, new in (([0], [1]), ([3], [2]), ([100], [1])):
+        for geo in ((2, 1, 128, "bf16"), (1, 1, 128, "f32"), (40, 1, 128, "bf16")):
+            _check(Case(15, cached, new, 16, *geo, pad_blocks=0))
 
 
 def test_many_requests_and_a_long_one():
@@ -186,9 +206,10 @@ def test_long_cache_offsets_beyond_32_bits():
     check_attend(c, 0, out, lse)
 
 
-def test_same_bits_every_time_on_any_stream_and_replayed():
+@pytest.mark.parametrize("geo,new", [(GEOS[0], [1, 1, 1]), (GEOS[0], [40, 1, 20]), (GEOS[5], [3, 1, 20]), (GEOS[7], [2, 1, 1])])
+def test_same_bits_every_time_on_any_stream_and_replayed(geo, new):
     from paper_2607_19547_amd import binding as b
-    c = Case(11, [3000, 100, 4500], [1, 1, 1], 64, 16, 2, 128)
+    c = Case(11, [3000, 100, 4500], new, 64, *geo)
     parts = c.dev(b)
     geo, pool, batch, q, out, lse = parts
     want, want_lse = (x.clone() for x in _run(c, parts=parts))
@@ -201,7 +222,8 @@ def test_same_bits_every_time_on_any_stream_and_replayed():
     with torch.cuda.graph(g):
         b.tree_attend_paged(geo, pool, 1, batch, q, out, lse, ws)
     lengths = batch.tensors[0]
-    for cached in ([3000, 100, 4500], [5, 0, 64], [3000, 100, 4500], [1, 4000, 17]):
+    # (the third request's table has room for its own length alone, the second's for 100 tokens and a page)
+    for cached in ([3000, 100, 4500], [5, 0, 64], [3000, 100, 4500], [1, 60, 17]):
         lengths.copy_(torch.tensor(cached, dtype=torch.int32))
         out.zero_()
         g.replay()
