@@ -111,7 +111,8 @@ __device__ __forceinline__ bool find_run(const SplitArgs& a, int w, Run* run) {
   int64_t sum = 0;
 #pragma unroll 4
   for (int b = b0; b < b1; ++b) sum += tiles(b);
-  const int64_t upto = wave_scan64(sum);
+  // (in 32 bits where the lanes' sums allow it: six steps of one instruction)
+  const int64_t upto = __ballot(sum >> 24) ? wave_scan64(sum) : (int64_t)wave_scan((unsigned)sum);
   const int64_t total = lane_value(upto, 63);
   const int64_t len = run_length(a, total), begin = w * len;
   if (begin >= total) return false;
