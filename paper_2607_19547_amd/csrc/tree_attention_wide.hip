@@ -13,6 +13,12 @@
 // (pages are multiples of 16 tokens); rows behind the request's end, and rows
 // of no page of the pool, read as zeros.
 //
+// Bound by the matrix instructions and the exponentials between them, at the
+// clock that their power leaves: two questions of 389 rows over 32,768 tokens, 16 /
+// 2 heads, 220 us, 0.95 PFLOP/s (1.02 with the rows that fill the last row tile; a
+// product of two 8,192 x 8,192 matrices runs at 1.11); about 2 us a tile.  Starting a
+// launch and leaving its pieces takes as long as 8 tiles.
+//
 // The work is cut as in the kernel for few rows (equal runs of key tiles, one
 // run for each of 256 workgroups, one workgroup per CU).  A piece of a unit
 // leaves its outputs, in the accumulators' own layout, divided by their sum and
