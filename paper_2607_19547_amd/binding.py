@@ -167,7 +167,7 @@ def _ptr(t):
 _raw_stream = None  # torch's lookup of a device's current stream as an address
 
 
-def _stream(stream):
+def _stream(stream, device=None):
     """The address of the stream given, or of torch's current one (looked up without making a
     Stream object where torch has that call: 0.3 us instead of 3)."""
     if stream is not None:
@@ -178,7 +178,7 @@ def _stream(stream):
         torch.cuda.current_stream()  # (initialises the runtime, and says why where it cannot)
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
             lambda device: torch.cuda.current_stream(device).cuda_stream)
-    return _raw_stream(torch.cuda.current_device())
+    return _raw_stream(torch.cuda.current_device() if device is None else device)
 
 
 def compose_rebase_k(geo, k_cache, chunk_offsets, local_coords=None, want_global=False, stream=None):
@@ -362,8 +362,8 @@ def _torch_dtype(dtype, _cache={}):
     return t
 
 
-def _array(t, name, dtype, shape, optional=False):
-    """Device address of a dense tensor of the given type and shape (None in the shape: any size)."""
+def _array(t, name, dtype, shape, device, optional=False):
+    """Address of a dense tensor of the given type and shape (None in the shape: any size) on a device (None: any)."""
     if t is None:
         if optional:
             return None
@@ -373,9 +373,13 @@ def _array(t, name, dtype, shape, optional=False):
             len(have) != len(shape) or any(w is not None and w != h for h, w in zip(have, shape)))):
         raise ValueError(f"{name} must be a contiguous {_torch_dtype(dtype)} tensor of shape {shape}, got {t.dtype} "
                          f"{tuple(have)}")
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be in device memory")
+    if not t.is_cuda or (device is not None and t.get_device() != device):
+        raise ValueError(f"{name} must be in the memory of the batch's device")
     return t.data_ptr()
+
+
+def _page_key(geo):
+    return geo.g.n_layers, geo.g.n_kv_heads, geo.g.n_tokens, geo.g.head_dim, geo.g.dtype
 
 
 class PagePool:
@@ -383,10 +387,11 @@ class PagePool:
 
     def __init__(self, geo, k_pages, v_pages):
         shape = (None, geo.g.n_layers, geo.g.n_kv_heads, geo.g.n_tokens, geo.g.head_dim)
-        self.tensors = (k_pages, v_pages)
+        self.tensors, self.geo = (k_pages, v_pages), geo
         self.c = _PagePool()
-        self.c.k_pages = _array(k_pages, "k_pages", geo.g.dtype, shape)
-        self.c.v_pages = _array(v_pages, "v_pages", geo.g.dtype, (k_pages.shape[0],) + shape[1:])
+        self.c.k_pages = _array(k_pages, "k_pages", geo.g.dtype, shape, None)
+        self.device = k_pages.get_device()
+        self.c.v_pages = _array(v_pages, "v_pages", geo.g.dtype, (k_pages.shape[0],) + shape[1:], self.device)
         self.c.n_pages = k_pages.shape[0]
 
 
@@ -400,12 +405,13 @@ class Batch:
         c = self.c = _Batch()
         c.n_requests, c.n_rows, c.max_blocks, c.max_rows = n, rows, block_table.shape[1], int(max_rows)
         c.mask_words = 0 if tree_mask is None else tree_mask.shape[1]
-        c.cached_len = _array(cached_len, "cached_len", "int32", (n,))
-        c.row_start = _array(row_start, "row_start", "int32", (n + 1,))
-        c.block_table = _array(block_table, "block_table", "int32", (n, None))
-        c.slot = _array(slot, "slot", "int32", (rows,))
-        c.coords = _array(coords, "coords", "int32", (rows, 3))
-        c.tree_mask = _array(tree_mask, "tree_mask", "int64", (rows, None), optional=True)
+        c.cached_len = _array(cached_len, "cached_len", "int32", (n,), None)
+        dev = self.device = cached_len.get_device()
+        c.row_start = _array(row_start, "row_start", "int32", (n + 1,), dev)
+        c.block_table = _array(block_table, "block_table", "int32", (n, None), dev)
+        c.slot = _array(slot, "slot", "int32", (rows,), dev)
+        c.coords = _array(coords, "coords", "int32", (rows, 3), dev)
+        c.tree_mask = _array(tree_mask, "tree_mask", "int64", (rows, None), dev, optional=True)
 
 
 class PagePlan:
@@ -418,16 +424,17 @@ class PagePlan:
         self.tensors = (new_len, n_blocks, n_blocks_out, free_pages, free_head, free_head_out, status, parent,
                         coord_base)
         c = self.c = _PagePlan()
-        c.new_len = _array(new_len, "new_len", "int32", (n,))
-        c.n_blocks = _array(n_blocks, "n_blocks", "int32", (n,))
-        c.n_blocks_out = _array(n_blocks_out, "n_blocks_out", "int32", (n,))
-        c.free_pages = _array(free_pages, "free_pages", "int32", (None,))
+        c.new_len = _array(new_len, "new_len", "int32", (n,), None)
+        dev = self.device = new_len.get_device()
+        c.n_blocks = _array(n_blocks, "n_blocks", "int32", (n,), dev)
+        c.n_blocks_out = _array(n_blocks_out, "n_blocks_out", "int32", (n,), dev)
+        c.free_pages = _array(free_pages, "free_pages", "int32", (None,), dev)
         c.n_free = free_pages.shape[0]
-        c.free_head = _array(free_head, "free_head", "int32", (1,))
-        c.free_head_out = _array(free_head_out, "free_head_out", "int32", (1,))
-        c.status = _array(status, "status", "int32", (1,))
-        c.parent = _array(parent, "parent", "int32", (None,), optional=True)
-        c.coord_base = _array(coord_base, "coord_base", "int32", (n,), optional=True)
+        c.free_head = _array(free_head, "free_head", "int32", (1,), dev)
+        c.free_head_out = _array(free_head_out, "free_head_out", "int32", (1,), dev)
+        c.status = _array(status, "status", "int32", (1,), dev)
+        c.parent = _array(parent, "parent", "int32", (None,), dev, optional=True)
+        c.coord_base = _array(coord_base, "coord_base", "int32", (n,), dev, optional=True)
         self.n_requests, self.n_parents = n, None if parent is None else parent.shape[0]
 
 
@@ -436,11 +443,24 @@ def _row_arg(t, name, geo, batch, heads):
     if isinstance(t, Rows):
         return t
     shape, d = t.shape, geo.g.head_dim
-    if t.dtype is not _torch_dtype(geo.g.dtype) or not t.is_cuda or len(shape) != 3 or (
+    if t.dtype is not _torch_dtype(geo.g.dtype) or t.get_device() != batch.device or len(shape) != 3 or (
             shape[0] < batch.c.n_rows or shape[1] != heads or shape[2] != d):
-        raise ValueError(f"{name} must be a {_torch_dtype(geo.g.dtype)} device tensor [{batch.c.n_rows}, {heads}, "
-                         f"{d}], got {t.dtype} {tuple(shape)}")
+        raise ValueError(f"{name} must be a {_torch_dtype(geo.g.dtype)} tensor [{batch.c.n_rows}, {heads}, {d}] on the "
+                         f"batch's device, got {t.dtype} {tuple(shape)}")
     return Rows.of(t)
+
+
+def _batch_stream(stream, batch, other, geo=None):
+    """The stream, after a look at the devices (the batch's, the pool's or plan's, the current one) and at the
+    pool's geometry, where one is given."""
+    import torch
+    device = torch.cuda.current_device()
+    if batch.device != device or other.device != device:
+        raise ValueError(f"the batch is on device {batch.device}, its pool or plan on {other.device}, and the current "
+                         f"device is {device}")
+    if geo is not None and geo is not other.geo and _page_key(geo) != _page_key(other.geo):
+        raise ValueError("the pool's pages are of another geometry")
+    return _stream(stream, device)
 
 
 def batch_plan_pages(geo, n_pages, batch, plan, stream=None):
@@ -448,20 +468,21 @@ def batch_plan_pages(geo, n_pages, batch, plan, stream=None):
     if plan.n_requests != batch.c.n_requests or plan.n_parents not in (None, batch.c.n_rows):
         raise ValueError("the plan's tensors are of another batch")
     _check(lib().batch_plan_pages(geo.ref, int(n_pages), ctypes.byref(batch.c), ctypes.byref(plan.c),
-                                  _stream(stream)))
+                                  _batch_stream(stream, batch, plan)))
 
 
 def qk_norm_rope_append(geo, pool, layer, batch, q, k, v, q_out, q_weight=None, k_weight=None, eps=1e-6,
                         stream=None):
     """Norm and rotation of the step's queries (to q_out) and keys; keys and values to their slots in `layer`."""
     hq, hkv = geo.g.n_q_heads, geo.g.n_kv_heads
-    w = [_array(x, "a weight", geo.g.dtype, (geo.g.head_dim,), optional=True)
+    w = [_array(x, "a weight", geo.g.dtype, (geo.g.head_dim,), batch.device, optional=True)
          for x in (q_weight, k_weight)]
     _check(lib().qk_norm_rope_append(geo.ref, ctypes.byref(pool.c), int(layer), ctypes.byref(batch.c),
                                      ctypes.byref(_row_arg(q, "q", geo, batch, hq)),
                                      ctypes.byref(_row_arg(k, "k", geo, batch, hkv)),
                                      ctypes.byref(_row_arg(v, "v", geo, batch, hkv)), w[0], w[1], float(eps),
-                                     ctypes.byref(_row_arg(q_out, "q_out", geo, batch, hq)), _stream(stream)))
+                                     ctypes.byref(_row_arg(q_out, "q_out", geo, batch, hq)),
+                                     _batch_stream(stream, batch, pool, geo)))
 
 
 def tree_attend_paged_workspace(geo, batch):
@@ -474,13 +495,15 @@ def tree_attend_paged(geo, pool, layer, batch, q, out, lse=None, workspace=None,
     """Attention of the step's rows over their requests' pages; lse: float32 [n_rows, H_q] or None."""
     hq = geo.g.n_q_heads
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    if workspace is not None and (workspace.get_device() != batch.device or not workspace.is_contiguous()):
+        raise ValueError("workspace must be contiguous memory of the batch's device")
     if lse is not None and lse.shape[0] < batch.c.n_rows:
         raise ValueError("lse has fewer rows than the batch")
     _check(lib().tree_attend_paged(geo.ref, ctypes.byref(pool.c), int(layer), ctypes.byref(batch.c),
                                    ctypes.byref(_row_arg(q, "q", geo, batch, hq)),
                                    ctypes.byref(_row_arg(out, "out", geo, batch, hq)),
-                                   _array(lse, "lse", "float32", (None, hq), optional=True), _ptr(workspace),
-                                   ws_bytes, _stream(stream)))
+                                   _array(lse, "lse", "float32", (None, hq), batch.device, optional=True),
+                                   _ptr(workspace), ws_bytes, _batch_stream(stream, batch, pool, geo)))
 
 
 def tree_commit_paged(geo, pool, layer_begin, layer_end, batch, accepted, n_accepted, cached_len_out=None,
@@ -488,7 +511,7 @@ def tree_commit_paged(geo, pool, layer_begin, layer_end, batch, accepted, n_acce
     """Moves the rows of accepted int32 [B, max_accept] (n_accepted [B] of them) behind the cached tokens."""
     n = batch.c.n_requests
     _check(lib().tree_commit_paged(geo.ref, ctypes.byref(pool.c), int(layer_begin), int(layer_end),
-                                   ctypes.byref(batch.c), _array(accepted, "accepted", "int32", (n, None)),
-                                   accepted.shape[1], _array(n_accepted, "n_accepted", "int32", (n,)),
-                                   _array(cached_len_out, "cached_len_out", "int32", (n,), optional=True),
-                                   _stream(stream)))
+                                   ctypes.byref(batch.c), _array(accepted, "accepted", "int32", (n, None), batch.device),
+                                   accepted.shape[1], _array(n_accepted, "n_accepted", "int32", (n,), batch.device),
+                                   _array(cached_len_out, "cached_len_out", "int32", (n,), batch.device, optional=True),
+                                   _batch_stream(stream, batch, pool, geo)))

@@ -203,7 +203,7 @@ __global__ __launch_bounds__(kAppendThreads) void qk_norm_rope_any(const AppendA
   }
 }
 
-constexpr double kOnceBytes = 128e6;
+constexpr double kOnceBytes = 96e6;
 template <typename E, int LH>
 static void run_vec(const AppendArgs& a, dim3 grid, size_t lds, TraceScope& tr, hipStream_t s) {
   constexpr int PV = 16 / sizeof(E);

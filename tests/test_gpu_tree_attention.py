@@ -249,3 +249,26 @@ def test_two_calls_at_once_with_workspaces_of_their_own():
     torch.cuda.synchronize()
     for p, w in zip(parts, want):
         assert torch.equal(p[4], w[0]) and torch.equal(p[5], w[1])
+
+
+def test_binding_refuses_other_memory_types_and_geometries():
+    from paper_2607_19547_amd import binding as b
+    c = Case(16, [30], [2], 16, 4, 2, 128)
+    geo, pool, batch, q, out, lse = c.dev(b)
+    ws = torch.empty(b.tree_attend_paged_workspace(geo, batch), dtype=torch.uint8, device="cuda")
+    call = lambda **kw: b.tree_attend_paged(kw.get("geo", geo), pool, 0, batch, kw.get("q", q), kw.get("out", out),
+                                            kw.get("lse", lse), kw.get("ws", ws))
+    call()
+    other = b.Geo(2, 8, 4, 128, (16, 24, 24), "bf16", [0, 16])
+    big = torch.zeros(2, 8, 128, dtype=torch.bfloat16, device="cuda")
+    for kw in (dict(q=q.cpu()), dict(q=q.float()), dict(q=q[:, :2]), dict(q=q[:1]), dict(out=out.cpu()), dict(lse=lse.cpu()),
+               dict(lse=lse.double()), dict(ws=ws.cpu()), dict(lse=lse[:1]), dict(geo=other, q=big, out=big, lse=None)):
+        with pytest.raises(ValueError):
+            call(**kw)
+    with pytest.raises(b.CsError) as e:
+        call(ws=ws[:8])
+    assert e.value.code == b.CS_ERR_WORKSPACE_TOO_SMALL
+    with pytest.raises(ValueError):
+        b.tree_commit_paged(geo, pool, 0, 2, batch, torch.zeros(1, 3, dtype=torch.int64, device="cuda"), batch.tensors[0])
+    with pytest.raises(ValueError):
+        b.Batch(*[t.cpu() if i == 2 else t for i, t in enumerate(batch.tensors[:5])])
