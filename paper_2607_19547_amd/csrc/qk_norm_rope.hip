@@ -7,7 +7,7 @@
 // heads, so a workgroup takes a few whole rows: its threads make the rows'
 // cos/sin tables in LDS, then groups of lanes take one head each.  Bound by
 // memory: a head is read once and written once (32,762 rows of 16 + 2 x 2 heads of
-// 128 in bf16: 61 us, 5.5 TB/s; 5,172 rows in float32: 21.6 us, 4.9 TB/s; one row:
+// 128 in bf16: 61 us, 5.5 TB/s; 5,172 rows in float32: 23.0 us, 4.6 TB/s; one row:
 // 3.1 us).  Four rows a workgroup make one table entry per thread.
 #include <algorithm>
 
@@ -203,7 +203,7 @@ __global__ __launch_bounds__(kAppendThreads) void qk_norm_rope_any(const AppendA
   }
 }
 
-constexpr double kOnceBytes = 96e6;
+constexpr double kOnceBytes = 128e6;
 template <typename E, int LH>
 static void run_vec(const AppendArgs& a, dim3 grid, size_t lds, TraceScope& tr, hipStream_t s) {
   constexpr int PV = 16 / sizeof(E);

@@ -374,12 +374,9 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const SplitArgs) {
             }
           }
         }
-      bool have[SUB], some = false;  // the 16 keys lie in a page of the pool
+      bool have[SUB];  // the 16 keys lie in a page of the pool
 #pragma unroll
-      for (int y = 0; y < SUB; ++y) {
-        have[y] = bytes[y] != 0;
-        some = some || have[y];
-      }
+      for (int y = 0; y < SUB; ++y) have[y] = bytes[y] != 0;
       places(tile + kWaves);
       load_k();
       fetch_pages(tile + 2 * kWaves);
@@ -390,8 +387,10 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const SplitArgs) {
 #pragma unroll
         for (int y = 0; y < SUB; ++y)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) p[x][4 * y + i] = fmaf(s[x][y][i], sc, have[y] ? 0.f : -INFINITY);
-      const bool masked = tile >= t_full;
+          for (int i = 0; i < 4; ++i) p[x][4 * y + i] = s[x][y][i];
+      bool masked = tile >= t_full;
+#pragma unroll
+      for (int y = 0; y < SUB; ++y) masked = masked || !have[y];
       uint32_t vis[NR];  // bit 16 y + i: key 16 y + 4 lg + i
       if (masked) {
         const SplitArgs A = args();
@@ -422,7 +421,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const SplitArgs) {
         }
       } else {
 #pragma unroll
-        for (int x = 0; x < NR; ++x) seen[x] = seen[x] || some;
+        for (int x = 0; x < NR; ++x) seen[x] = true;
       }
 
 #pragma unroll
@@ -430,7 +429,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const SplitArgs) {
         float mx = p[x][0];
 #pragma unroll
         for (int j = 1; j < NS; ++j) mx = fmaxf(mx, p[x][j]);
-        mx = group_max(mx);
+        mx = group_max(mx) * sc;
         const bool grow = mx > m[x] + kRescaleLog2;
         if (__ballot(grow)) {
           const float m_new = grow ? mx : m[x];
@@ -443,7 +442,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const SplitArgs) {
         const float ref = m[x] == -INFINITY ? 0.f : m[x];
 #pragma unroll
         for (int j = 0; j < NS; ++j) {
-          p[x][j] = __builtin_amdgcn_exp2f(p[x][j] - ref);
+          p[x][j] = __builtin_amdgcn_exp2f(fmaf(p[x][j], sc, -ref));
           l[x] += p[x][j];
         }
       }

@@ -15,7 +15,7 @@
 //
 // Bound by the matrix instructions and the exponentials between them, at the
 // clock that their power leaves: two questions of 389 rows over 32,768 tokens, 16 /
-// 2 heads, 220 us, 0.95 PFLOP/s (1.02 with the rows that fill the last row tile; a
+// 2 heads, 210 us, 1.0 PFLOP/s (1.07 with the rows that fill the last row tile; a
 // product of two 8,192 x 8,192 matrices runs at 1.11); about 2 us a tile.  Starting a
 // launch and leaving its pieces takes as long as 8 tiles.
 //
