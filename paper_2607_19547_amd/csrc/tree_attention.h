@@ -48,7 +48,8 @@ struct SplitArgs {
   TreeArgs t;
   float* part;      // [2 workgroups][row tile][D] unnormalised partial outputs
   float* part_ml;   // [2 workgroups][row tile][2] their maximum (log2 units) and sum
-  int min_tiles;    // key tiles of a run at least
+  int min_tiles;    // key tiles of a run at least, where the units are that long
+  FastDiv units;    // division by the units that there are about: the rows shared out evenly
   int row_bits;     // a row tile has 2^row_bits query vectors
   int tile_bits;    // a key tile has 2^tile_bits keys
   int run_bits;     // 2^run_bits runs at most
@@ -78,8 +79,12 @@ __device__ __forceinline__ int unit_at(int64_t off, int ntile, int* tile) {
   return u;
 }
 // Key tiles of a run: the same for all, so that run w is [w x len, (w + 1) x len).
+// A run of min_tiles pays for what its unit costs beside the tiles; where units
+// are shorter than that, one costs as much by itself, and a run has one of them.
 __device__ __forceinline__ int64_t run_length(const SplitArgs& a, int64_t total) {
-  return max((int64_t)a.min_tiles, (total + (1 << a.run_bits) - 1) >> a.run_bits);
+  int at_least = a.min_tiles;
+  if (total < (int64_t)a.min_tiles * a.units.d) at_least = a.units.div((int)total + a.units.d - 1);
+  return max((int64_t)at_least, (total + (1 << a.run_bits) - 1) >> a.run_bits);
 }
 
 struct Run {
@@ -177,12 +182,18 @@ struct Merge {
   __device__ __forceinline__ float lse() const { return (m + __log2f(sum)) * kLn2; }
 };
 
+// Units of a batch whose requests have all as many rows.
+inline int even_units(const SplitArgs& a) {
+  const int64_t vectors = (int64_t)a.t.n_rows * a.t.G, per_tile = (int64_t)a.t.B << a.row_bits;
+  const int64_t units = std::max<int64_t>(1, (vectors + per_tile - 1) / per_tile) * a.t.B * a.t.Hkv;
+  return (int)std::min<int64_t>(units, 1 << 26);  // (times min_tiles in 32 bits: more has runs enough)
+}
 // Workgroups that a launch needs at most: the runs there can be, from the rows
 // and the block tables' room.  A batch with room for one run needs no merge.
 inline int most_runs(const SplitArgs& a) {
   const double tiles = std::max<double>(1, ((double)a.t.max_blocks * a.t.page.d + (1 << a.tile_bits) - 1) / (1 << a.tile_bits));
   const double units = ((double)a.t.n_rows * a.t.G / (1 << a.row_bits) + a.t.B) * a.t.Hkv;
-  return (int)std::min<double>(1 << a.run_bits, ceil(tiles * units / a.min_tiles) + 1);
+  return (int)std::min<double>(1 << a.run_bits, std::max<double>(a.units.d, ceil(tiles * units / a.min_tiles)));
 }
 
 // The instance for many rows (bf16, head_dim 128): see tree_attention_wide.hip.

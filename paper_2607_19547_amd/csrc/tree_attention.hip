@@ -231,7 +231,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const SplitArgs) {
     const int i_last = a.group.div(min(rt * RT + RT, vectors) - 1);
     const int key_end = t.mask ? q.len : min(q.len, q.cached + i_last + 1);
     const int t_end = min(t0 + seg, (key_end + KT - 1) / KT);
-    const int t_full = min(q.cached, q.len) / KT;  // tiles before it: every row sees every key
+    const int t_full = min(t.mask ? q.cached : q.cached + a.group.div(rt * RT) + 1, q.len) / KT;  // tiles before it: every row sees every key
 
     Words<16> qf[NR][KS];
     int row[NR];  // the lane's row in the request, per 16 query vectors
@@ -680,19 +680,24 @@ static double room_bytes(const Geo& g, const cs_batch& b) {  // of the keys and 
 }
 static int row_groups(const Geo& g, const cs_batch& b) {
   const int64_t qv = query_vectors(g, b);
-  if (qv <= (wide_type(g) ? 32 : 16) || g.D > 128) return 1;
+  if (qv <= 16 || g.D > 128) return 1;
   const double row_bytes = g.D * g.esize;
   if (room_bytes(g, b) * ((qv + 15) / 16) < 1.6 * (50e6 + 0.3e6 * row_bytes)) return 1;
   return qv <= 256 || row_bytes > 128 ? 2 : 4;
 }
 
 // Whether the kernel for many rows takes the batch (where its pointers are
-// aligned).  Measured (us, with 16 query vectors a row tile / that kernel), 8
-// query heads a KV head: 65,000 tokens, 4 rows 27 / 22, 16 rows 79 / 23; 16
-// requests of up to 4,000 tokens, 4 rows 20 / 20, 16 rows 31 / 21; 8,000 tokens, 4
-// rows 14 / 17, 16 rows 16 / 17.
+// aligned): it reads the keys and values once for 256 query vectors and has more to
+// do before its first tile.  Measured (us, row tiles of 16 query vectors / that
+// kernel), by what the row tiles of 16 read in all: 35 MB (4,000 tokens, 3 rows, 8
+// query heads for each of 8 KV heads) 16 / 23; 69 MB (4,000 tokens, 32 rows, 8 for
+// each of 2) 20 / 27; 119 MB (8 requests of 1,000 tokens, 5 rows, 8 for each of 8)
+// 27 / 23; 134 MB (65,000 tokens, 3 rows, 8 for each of 2) 30 / 29; 277 MB (8
+// requests of 4,000 tokens, 4 rows, 8 for each of 8) 50 / 37; 1.1 GB (32 of them) 160
+// / 103.  (The room is seldom filled.)
 static bool wide(const Geo& g, const cs_batch& b) {
-  return wide_type(g) && g.T % 16 == 0 && query_vectors(g, b) > 32;
+  const int64_t row_tiles = (query_vectors(g, b) + 15) / 16;
+  return wide_type(g) && row_tiles > 1 && room_bytes(g, b) * row_tiles >= 150e6;
 }
 
 size_t tree_attend_workspace(const Geo& g, const cs_batch& b) {
@@ -774,6 +779,7 @@ cs_status launch_tree_attend(const Geo& g, const cs_page_pool& pool, int layer, 
   a.tile_bits = g.dtype == CS_BF16 ? 5 : 4;
   a.min_tiles = 2 * kWaves;
   a.run_bits = kRunBits;
+  a.units = fast_div(even_units(a));
   a.part = (float*)(((uintptr_t)ws + 255) & ~(uintptr_t)255);
   a.part_ml = a.part + 2 * ((size_t)kRuns << a.row_bits) * g.D;
   if (g.dtype == CS_BF16) {

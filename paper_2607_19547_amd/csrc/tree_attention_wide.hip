@@ -139,7 +139,8 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
     t0 = uniform(t0);
     const int seg = (int)min(left, (int64_t)(ntile - t0));
     const int h = uniform(u / nrt), rt = u - h * nrt;
-    int n_kt, key_begin, g_row, w_seen, bad;  // g_row: the lane's row; w_seen: keys behind it are seen by no row of the wavefront
+    // all_see: keys that every row sees; g_row: the lane's row; w_seen: keys behind it are seen by no row of the wavefront
+    int n_kt, key_begin, all_see, g_row, w_seen, bad;
     bf16x8 qb[8];
     {
       const SplitArgs A = args();
@@ -147,6 +148,7 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
       // rows see no key behind their own without a mask, so later tiles are left out
       const int i_last = A.group.div(min((rt + 1) * 256, vectors) - 1);
       const int key_end = A.t.mask ? q.len : min(q.len, q.cached + i_last + 1);
+      all_see = min(A.t.mask ? q.cached : q.cached + A.group.div(rt * 256) + 1, q.len);
       key_begin = t0 * kKT;
       n_kt = max(min(t0 + seg, (key_end + kKT - 1) / kKT) - t0, 0);
       const int v0 = rt * 256 + 32 * wave;
@@ -413,7 +415,7 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
     // First the tiles that every row sees whole, their ring slots known to the
     // compiler, a tile's scores computed a step ahead; then, in a plain loop, the
     // few with the step's own rows.
-    const int n_clear = bad ? 0 : min(max(min(q.cached, q.len) / kKT - t0, 0), n_kt);
+    const int n_clear = bad ? 0 : min(max(all_see / kKT - t0, 0), n_kt);
     f32x16 sa0, sa1, sb0, sb1;
     asm volatile("s_waitcnt vmcnt(4)" ::: "memory");  // tiles 0 and 1 and the queries have landed
     __builtin_amdgcn_s_barrier();
@@ -606,6 +608,7 @@ void launch_tree_wide(SplitArgs a, void* ws, bool once, hipStream_t s) {
   a.tile_bits = kWideTileBits;
   a.run_bits = kWideRunBits;
   a.min_tiles = 4;
+  a.units = fast_div(even_units(a));
   a.part = (float*)(((uintptr_t)ws + 255) & ~(uintptr_t)255);
   a.part_ml = a.part + 2 * (size_t)kWideRuns * kPartHalfs / 2;
   const int runs = most_runs(a);

@@ -64,6 +64,13 @@ class Case:
         self.words = max(1, -(-max(new, default=1) // 64))
         self.ob = ob
 
+    def roomy(self):
+        """The same batch with block tables of so much room that several rows take the kernel for many."""
+        blocks = int(120e6) // (max(len(self.new), 1) * self.page * self.hkv * self.d * 4) + 1
+        self.table = np.pad(self.table, ((0, 0), (0, blocks)), constant_values=-1)
+        self.max_blocks += blocks
+        return self
+
     def geo(self, b):
         return b.Geo(self.layers, self.hq, self.hkv, self.d, sections(self.d), self.dtype, [0, self.page])
 

@@ -30,6 +30,8 @@ def _check(c, layer=1, **kw):
     out, lse = _run(c, layer, **kw)
     check_attend(c, layer, out, lse, f"{c.cached} + {c.new}, page {c.page}, {c.hq}/{c.hkv} x {c.d} {c.dtype}")
     assert (out[c.rows:] == 7).all() and (lse[c.rows:] == 7).all(), "rows behind the last request changed"
+    if c.d == 128 and c.dtype == "bf16" and c.max_blocks < 1000:  # with the kernel for many rows too
+        _check(c.roomy(), layer, **kw)
 
 
 SHAPES = [  # cached, new, page
@@ -123,11 +125,13 @@ def test_pages_outside_the_pool_are_not_seen():
         _check(c)
 
 
-@pytest.mark.parametrize("geo", [GEOS[0], GEOS[5], GEOS[7]])
-def test_arrays_that_are_no_plans(geo):
+@pytest.mark.parametrize("geo,room", [(GEOS[0], False), (GEOS[0], True), (GEOS[5], False), (GEOS[7], False)])
+def test_arrays_that_are_no_plans(geo, room):
     """Row starts and lengths out of range: bounded, nothing else is touched."""
     from paper_2607_19547_amd import binding as b
     c = Case(6, [20, 30], [4, 4], 16, *geo, pad_rows=2)
+    if room:
+        c.roomy()
     parts = c.dev(b)
     for start, cached in (([0, 4, 1 << 30], [20, 30]), ([0, 9, 3], [20, 30]), ([-5, 4, 8], [-3, 1 << 30]),
                           ([0, 4, 8], [0x7fffffff, 30])):
@@ -181,6 +185,15 @@ def test_short_batches_of_one_piece():
             _check(Case(15, cached, new, 16, *geo, pad_blocks=0))
 
 
+@pytest.mark.parametrize("geo", [GEOS[0], GEOS[1], GEOS[2], GEOS[4], GEOS[6]])
+@pytest.mark.parametrize("new", [1, 3, 40])
+def test_units_shorter_than_a_run(geo, new):
+    """Requests of a few keys each: a run has one of their units, or, where there are more than runs, some."""
+    for seed, (n, cached) in enumerate(((2, 3), (40, 20), (9, 300))):
+        lengths = np.random.default_rng(seed).integers(0, cached + 1, n).tolist()
+        _check(Case(16, lengths, [(new * (b + 1)) % (new + 1) for b in range(n)], 16, *geo, layers=1, pad_rows=1), 0)
+
+
 def test_many_requests_and_a_long_one():
     rng = np.random.default_rng(9)
     cached = rng.integers(0, 40, 300).tolist()
@@ -206,10 +219,13 @@ def test_long_cache_offsets_beyond_32_bits():
     check_attend(c, 0, out, lse)
 
 
-@pytest.mark.parametrize("geo,new", [(GEOS[0], [1, 1, 1]), (GEOS[0], [40, 1, 20]), (GEOS[5], [3, 1, 20]), (GEOS[7], [2, 1, 1])])
-def test_same_bits_every_time_on_any_stream_and_replayed(geo, new):
+@pytest.mark.parametrize("geo,new,room", [(GEOS[0], [1, 1, 1], False), (GEOS[0], [40, 1, 20], False), (GEOS[0], [40, 1, 20], True),
+                                          (GEOS[5], [3, 1, 20], False), (GEOS[7], [2, 1, 1], False)])
+def test_same_bits_every_time_on_any_stream_and_replayed(geo, new, room):
     from paper_2607_19547_amd import binding as b
     c = Case(11, [3000, 100, 4500], new, 64, *geo)
+    if room:
+        c.roomy()
     parts = c.dev(b)
     geo, pool, batch, q, out, lse = parts
     want, want_lse = (x.clone() for x in _run(c, parts=parts))
@@ -238,6 +254,7 @@ def test_same_bits_every_time_on_any_stream_and_replayed(geo, new):
 def test_two_calls_at_once_with_workspaces_of_their_own():
     from paper_2607_19547_amd import binding as b
     cases = [Case(s, [2500, 900], [n, n], 64, 16, 2, 128) for s, n in ((12, 1), (13, 40))]
+    cases[1].roomy()
     parts = [c.dev(b) for c in cases]
     want = [[x.clone() for x in _run(c, parts=p)] for c, p in zip(cases, parts)]
     ws = [torch.empty(max(1, b.tree_attend_paged_workspace(p[0], p[2])), dtype=torch.uint8, device="cuda") for p in parts]
