@@ -769,7 +769,7 @@ cs_status launch_tree_attend(const Geo& g, const cs_page_pool& pool, int layer, 
   }
   if (check_only) return CS_OK;
   a.group = fast_div(g.G);
-  if (wide(g, b) && low_o % 8 == 0) {
+  if (wide(g, b) && low_o % 16 == 0) {
     launch_tree_wide(a, ws, query_vectors(g, b) <= 256 && room_bytes(g, b) >= kWideOnceBytes, s);
     return check_launch("tree attention launch");
   }
