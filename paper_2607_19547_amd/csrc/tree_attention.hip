@@ -173,6 +173,30 @@ __device__ __forceinline__ float group_sum(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// The place of a run's next key tile, `off` of request b with `left` to go, past
+// requests' ends and the empty ends of pairs; n is 0 behind the last.  (A loop of
+// its own: two ways back to the loop over the pieces cost 34 registers.)
+template <bool PAIRS>
+__device__ __forceinline__ Place next_place(const SplitArgs& a, int* b, int64_t* off, int64_t* left, Request* q) {
+  Place x;
+  x.n = 0;
+#pragma unroll 1
+  while (*b < a.t.B && *left > 0) {
+    *q = load_request_scalar(a.t, *b);
+    const Units units = unit_sizes<PAIRS>(a, *q);
+    if (*off >= request_tiles(a, units)) {
+      *off = 0;
+      ++*b;
+      continue;
+    }
+    x = place_at<PAIRS>(a, *q, units, *off);
+    if (x.n) break;
+    *off += x.t0;
+    *left -= x.t0;
+  }
+  return x;
+}
+
 template <typename E, int D, int NR, bool ONCE>
 __global__ __launch_bounds__(kThreads, 2) void tree_attend(const SplitArgs) {
   constexpr bool kBf16 = sizeof(E) == 2;
@@ -204,7 +228,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const SplitArgs) {
     return *(const SplitArgs*)p;
   };
   Run run;
-  if (!find_run(args(), blockIdx.x, &run)) return;
+  if (!find_run<(NR > 1)>(args(), blockIdx.x, &run)) return;
   int64_t left = run.end - run.begin, off = run.off;
   int b = run.b;
   bool first_seg = true;
@@ -212,20 +236,11 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const SplitArgs) {
   while (left > 0) {
     const SplitArgs a = args();
     const TreeArgs& t = a.t;
-    if (b >= t.B) break;  // (lengths that changed meanwhile)
-    const Request q = load_request_scalar(t, b);
-    int nrt, ntile;
-    unit_sizes(a, q, &nrt, &ntile);
-    if (off >= (int64_t)t.Hkv * nrt * ntile) {  // behind this request's units
-      off = 0;
-      ++b;
-      continue;
-    }
-    int t0;
-    const int u = uniform(unit_at(off, ntile, &t0));
-    t0 = uniform(t0);
+    Request q;
+    const Place place = next_place<(NR > 1)>(a, &b, &off, &left, &q);
+    if (!place.n) break;
+    const int h = place.h, rt = place.rt, t0 = place.t0, ntile = place.n;
     const int seg = (int)min(left, (int64_t)(ntile - t0));
-    const int h = nrt == 1 ? u : uniform(u / nrt), rt = u - h * nrt;
     const int vectors = q.n * t.G;
     // rows see no key behind their own without a mask, so later tiles are left out
     const int i_last = a.group.div(min(rt * RT + RT, vectors) - 1);
@@ -510,7 +525,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const SplitArgs) {
     }
 
     // The wavefronts' results, 16 query vectors at a time, merged through LDS.
-    const int64_t slot = 2 * (int64_t)blockIdx.x + (first_seg ? 0 : 1);
+    const int64_t slot = 2 * (int64_t)blockIdx.x + (t0 == 0);  // (of a run's pieces, its first begins inside a row tile, its last ends there)
 #pragma unroll
     for (int x = 0; x < NR; ++x) {
       float lt = group_sum(l[x]);
@@ -581,24 +596,21 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const SplitArgs) {
 constexpr int kGroups = kThreads / 32;
 constexpr int kManyPieces = 16;
 constexpr int kRound = 8;  // pieces of a round
-template <typename E, int D>
+template <typename E, int D, bool PAIRS>
 __global__ __launch_bounds__(kThreads) void tree_combine(const SplitArgs a) {
   constexpr int C = (D + 31) / 32;  // elements a lane holds
   __shared__ float s_o[kGroups][32 * C], s_m[kGroups], s_l[kGroups];
   const TreeArgs& t = a.t;
   const int w1 = blockIdx.x + 1;
   Run run;
-  if (!find_run(a, w1, &run)) return;
+  if (!find_run<PAIRS>(a, w1, &run)) return;
   const Request q = load_request_scalar(t, run.b);
-  int nrt, ntile, tile;
-  unit_sizes(a, q, &nrt, &ntile);
-  const int u = unit_at(run.off, ntile, &tile);
-  if (tile == 0) return;  // the border lies between units
-  const int64_t len = run_length(a, run.total), unit0 = run.begin - tile, unit1 = unit0 + ntile;
+  const Place at = place_at<PAIRS>(a, q, unit_sizes<PAIRS>(a, q), run.off);
+  if (at.t0 == 0 || at.n == 0) return;  // the border lies between row tiles
+  const int h = at.h, rt = at.rt;
+  const int64_t len = run_length(a, run.total), unit0 = run.begin - at.t0, unit1 = unit0 + at.n;
   const int w0 = quotient(unit0, len), w_last = quotient(unit1 - 1, len);  // the runs of its first and last tile
   const int pieces = w_last - w0 + 1, borders = pieces - 1;
-  const int first = w0 * len < unit0 ? 1 : 0;  // the first piece ends its run, unless the run begins with the unit
-  const int h = u / nrt, rt = u - h * nrt;
   const int vectors = min(1 << a.row_bits, q.n * t.G - (rt << a.row_bits));
   const int grp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const bool many = pieces > kManyPieces;
@@ -613,7 +625,7 @@ __global__ __launch_bounds__(kThreads) void tree_combine(const SplitArgs a) {
 #pragma unroll
       for (int y = 0; y < kRound; ++y) {
         const int x = min(c + y * step, pieces - 1);
-        const int64_t at = ((2 * (int64_t)(w0 + x) + (x == 0 ? first : 0)) << a.row_bits) + r;
+        const int64_t at = ((2 * (int64_t)(w0 + x) + (x == 0)) << a.row_bits) + r;
         ml[y] = *(const float2*)(a.part_ml + at * 2);
         const float* pp = a.part + at * D + lane * C;
 #pragma unroll
@@ -716,7 +728,7 @@ static void run_split(const SplitArgs& a, hipStream_t s) {
   }
   if (runs == 1) return;
   TraceScope tr("tree_combine", s);
-  CS_LAUNCH(tr, (tree_combine<E, D>), dim3(runs - 1, 2 * NR), dim3(kThreads), 0, s, a);
+  CS_LAUNCH(tr, (tree_combine<E, D, (NR > 1)>), dim3(runs - 1, 2 * NR), dim3(kThreads), 0, s, a);
 }
 template <typename E, int D>
 static void run_split(const SplitArgs& a, int nr, bool once, hipStream_t s) {

@@ -94,10 +94,9 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, ql = lane & 31, hi = lane >> 5;
 
   Run run;
-  if (!find_run(a0, blockIdx.x, &run)) return;
+  if (!find_run<true>(a0, blockIdx.x, &run)) return;
   int64_t left = run.end - run.begin, off = run.off;
   int b = run.b;
-  bool first_seg = true;
 
   int koff[8];  // K operand: row ql, chunk 2s + hi (row 32 + ql has the same swizzle)
 #pragma unroll
@@ -123,22 +122,29 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
 
   while (left > 0) {
     Request q;
-    int u, t0, nrt, ntile;
+    int h, rt, t0, ntile;
     {
       const SplitArgs A = args();
       if (b >= A.t.B) break;  // (lengths that changed meanwhile)
       q = load_request_scalar(A.t, b);
-      unit_sizes(A, q, &nrt, &ntile);
-      if (off >= (int64_t)A.t.Hkv * nrt * ntile) {  // behind this request's units
+      const Units units = unit_sizes<true>(A, q);
+      if (off >= request_tiles(A, units)) {  // behind this request's units
         off = 0;
         ++b;
         continue;
       }
+      const Place place = place_at<true>(A, q, units, off);
+      h = place.h;
+      rt = place.rt;
+      t0 = place.t0;
+      ntile = place.n;
+      if (!ntile) {  // the empty end of a pair
+        off += t0;
+        left -= t0;
+        continue;
+      }
     }
-    u = uniform(unit_at(off, ntile, &t0));
-    t0 = uniform(t0);
     const int seg = (int)min(left, (int64_t)(ntile - t0));
-    const int h = uniform(u / nrt), rt = u - h * nrt;
     // all_see: keys that every row sees; g_row: the lane's row; w_seen: keys behind it are seen by no row of the wavefront
     int n_kt, key_begin, all_see, g_row, w_seen, bad;
     bf16x8 qb[8];
@@ -289,7 +295,9 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
     // are rescaled for the tile: their first factor is 0.)
     auto not_finite = [&](char* V, int kt) {
       uint32_t odd = 0;
-      for (int x = lane; x < kKT * kRow / 16; x += 64) {
+      int x = lane;
+      asm volatile("" : "+v"(x));  // (worked out here, not kept through the tiles)
+      for (; x < kKT * kRow / 16; x += 64) {
         const u32x4 v = *(const u32x4*)(V + 16 * x);
 #pragma unroll
         for (int y = 0; y < 4; ++y) odd |= (v[y] & 0x7f807f80u) + 0x00800080u;
@@ -496,7 +504,7 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
           *(u32x4*)((uint16_t*)A.t.out + (int64_t)(q.r0 + i) * A.t.o_row + (h * A.t.G + v - i * A.t.G) * A.t.o_head + 8 * (at & 15)) = w;
       }
     } else {
-      const int64_t slot = 2 * (int64_t)blockIdx.x + (first_seg ? 0 : 1);
+      const int64_t slot = 2 * (int64_t)blockIdx.x + (t0 == 0);
       float amax = 0.f;
 #pragma unroll
       for (int d = 0; d < 4; ++d)
@@ -520,7 +528,6 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
           *(f16x8*)(pp + (2 * d + r) * 512) = w;
         }
     }
-    first_seg = false;
     left -= seg;
     off += seg;
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -541,17 +548,15 @@ __global__ __launch_bounds__(kStripThreads) void tree_combine_wide(const SplitAr
   const TreeArgs& t = a.t;
   const int w1 = blockIdx.x + 1;
   Run run;
-  if (!find_run(a, w1, &run)) return;
+  if (!find_run<true>(a, w1, &run)) return;
   const Request q = load_request_scalar(t, run.b);
-  int nrt, ntile, tile;
-  unit_sizes(a, q, &nrt, &ntile);
-  const int u = unit_at(run.off, ntile, &tile);
-  if (tile == 0) return;  // the border lies between units
-  const int64_t len = run_length(a, run.total), unit0 = run.begin - tile;
-  const int w0 = quotient(unit0, len), w_last = quotient(unit0 + ntile - 1, len);
+  const Place at = place_at<true>(a, q, unit_sizes<true>(a, q), run.off);
+  if (at.t0 == 0 || at.n == 0) return;  // the border lies between row tiles
+  const int h = at.h, rt = at.rt;
+  const int64_t len = run_length(a, run.total), unit0 = run.begin - at.t0;
+  const int w0 = quotient(unit0, len), w_last = quotient(unit0 + at.n - 1, len);
   const int pieces = w_last - w0 + 1, borders = pieces - 1;
-  const int first = w0 * len < unit0 ? 1 : 0;
-  const int h = u / nrt, rt = u - h * nrt, vectors = min(256, q.n * t.G - rt * 256);
+  const int vectors = min(256, q.n * t.G - rt * 256);
   const int lane = threadIdx.x & 63, ql = lane & 31, hi = lane >> 5, grp = uniform(threadIdx.x >> 6);
   const bool many = pieces > kRound;
   const int step = many ? 4 : 1, strips = (vectors + 31) / 32 * 8;
@@ -565,7 +570,7 @@ __global__ __launch_bounds__(kStripThreads) void tree_combine_wide(const SplitAr
 #pragma unroll
       for (int y = 0; y < kRound; ++y) {
         const int x = min(x0 + y * step, pieces - 1);
-        const int64_t slot = 2 * (int64_t)(w0 + x) + (x == 0 ? first : 0);
+        const int64_t slot = 2 * (int64_t)(w0 + x) + (x == 0);
         st[y] = *(const float4*)(a.part_ml + (slot * 256 + r) * 4);
         v16[y] = *(const f16x8*)((const _Float16*)a.part + slot * kPartHalfs + strip * 512 + lane * 8);
       }

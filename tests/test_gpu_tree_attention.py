@@ -194,6 +194,19 @@ def test_units_shorter_than_a_run(geo, new):
         _check(Case(16, lengths, [(new * (b + 1)) % (new + 1) for b in range(n)], 16, *geo, layers=1, pad_rows=1), 0)
 
 
+@pytest.mark.parametrize("geo,new", [((4, 2, 128, "bf16"), [720, 1, 613]), (GEOS[2], [400, 5, 530]), (GEOS[4], [500, 0, 600]), (GEOS[5], [300, 2, 313])])
+def test_long_chains(geo, new):
+    """Row tiles that see few and many keys, taken in pairs (where requests are many, some here without
+    rows): with and without a cache, of odd and even numbers."""
+    from paper_2607_19547_amd import binding as b
+    c = Case(17, [0, 700, 333] + [0] * 37, new + [0] * 37, 64, *geo, layers=1, pad_rows=3).roomy()
+    _check(c, 0)
+    parts = c.dev(b)  # and lengths and a chain that a plan would not give
+    for cached in (0x7fffffff, -5):
+        parts[2].tensors[0].copy_(torch.tensor([cached, 700, cached] + [0] * 37, dtype=torch.int32))
+        _run(c, 0, parts=parts)
+
+
 def test_many_requests_and_a_long_one():
     rng = np.random.default_rng(9)
     cached = rng.integers(0, 40, 300).tolist()
