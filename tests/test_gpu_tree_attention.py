@@ -26,12 +26,12 @@ def _run(c, layer=1, max_rows=0, ws=None, q=None, out=None, lse=True, stream=Non
     return (out0 if out is None else out), lse0
 
 
-def _check(c, layer=1, **kw):
+def _check(c, layer=1, again=True, **kw):
     out, lse = _run(c, layer, **kw)
     check_attend(c, layer, out, lse, f"{c.cached} + {c.new}, page {c.page}, {c.hq}/{c.hkv} x {c.d} {c.dtype}")
     assert (out[c.rows:] == 7).all() and (lse[c.rows:] == 7).all(), "rows behind the last request changed"
-    if c.d == 128 and c.dtype == "bf16" and c.max_blocks < 1000:  # with the kernel for many rows too
-        _check(c.roomy(), layer, **kw)
+    if again and c.d == 128 and c.dtype == "bf16":  # with the kernel for many rows too
+        _check(c.roomy(), layer, again=False, **kw)
 
 
 SHAPES = [  # cached, new, page
@@ -200,7 +200,7 @@ def test_long_chains(geo, new):
     rows): with and without a cache, of odd and even numbers."""
     from paper_2607_19547_amd import binding as b
     c = Case(17, [0, 700, 333] + [0] * 37, new + [0] * 37, 64, *geo, layers=1, pad_rows=3).roomy()
-    _check(c, 0)
+    _check(c, 0, again=False)
     parts = c.dev(b)  # and lengths and a chain that a plan would not give
     for cached in (0x7fffffff, -5):
         parts[2].tensors[0].copy_(torch.tensor([cached, 700, cached] + [0] * 37, dtype=torch.int32))
