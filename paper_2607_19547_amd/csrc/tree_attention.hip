@@ -122,10 +122,11 @@ __global__ __launch_bounds__(kAnyThreads) void tree_attend_any(const TreeArgs a)
 // vectors a KV head: 155 us, 106 TFLOP/s).
 // The work, in key tiles over all units, is cut into equal runs, one for each
 // workgroup, whatever the requests' lengths: a run ends inside a unit or spans
-// several.  A unit that one workgroup has whole is finished there; of the
-// others each piece leaves a partial (O, max, sum), and tree_combine merges
-// them in key order, so results do not depend on timing.  Every workgroup
-// finds its run from the lengths alone (one load and a prefix sum).
+// several (a unit is a row tile, or two of a long chain: see Units).  A row tile
+// that one workgroup has whole is finished there; of the others each piece leaves
+// a partial (O, max, sum), and tree_combine merges them in key order, so results do
+// not depend on timing.  Every workgroup finds its run from the lengths alone (one
+// load and a prefix sum).
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 // The running maximum may grow by 2^5 before the accumulators are rescaled:

@@ -481,6 +481,7 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
       // 8 bytes, a row each: 61 questions of 388 rows 157 us, so 146).
       // A wavefront has 8 KB of the ring to itself, chunk c of a row at c ^ (row & 15).
       __builtin_amdgcn_s_barrier();  // the last loads of every wavefront have landed
+      asm volatile("" ::: "memory");
       const float inv = m_use == -INFINITY && lt == 0.f ? 0.f : 1.f / lt;
       char* rows = v_at(wave >> 1) + (wave & 1) * 32 * kRow;
       int at = lane;
@@ -532,6 +533,7 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
     off += seg;
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();  // the ring is free (the stores need not have landed)
+    asm volatile("" ::: "memory");
   }
 }
 
