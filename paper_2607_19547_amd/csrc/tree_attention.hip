@@ -229,7 +229,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const SplitArgs) {
     return *(const SplitArgs*)p;
   };
   Run run;
-  if (!find_run<(NR > 1)>(args(), blockIdx.x, &run)) return;
+  if (!find_run<(NR > 1), (NR > 1)>(args(), blockIdx.x, &run)) return;
   int64_t left = run.end - run.begin, off = run.off;
   int b = run.b;
   bool first_seg = true;
@@ -526,7 +526,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const SplitArgs) {
     }
 
     // The wavefronts' results, 16 query vectors at a time, merged through LDS.
-    const int64_t slot = 2 * (int64_t)blockIdx.x + (t0 == 0);  // (of a run's pieces, its first begins inside a row tile, its last ends there)
+    const int64_t slot = 2 * (int64_t)run.w + (t0 == 0);  // (of a run's pieces, its first begins inside a row tile, its last ends there)
 #pragma unroll
     for (int x = 0; x < NR; ++x) {
       float lt = group_sum(l[x]);
@@ -725,7 +725,7 @@ static void run_split(const SplitArgs& a, hipStream_t s) {
   const int runs = most_runs(a);
   {
     TraceScope tr("tree_attend", s);
-    CS_LAUNCH(tr, (tree_attend<E, D, NR, ONCE>), dim3(runs), dim3(kThreads), 0, s, a);
+    CS_LAUNCH(tr, (tree_attend<E, D, NR, ONCE>), dim3(NR > 1 ? (runs + 7) / 8 * 8 : runs), dim3(kThreads), 0, s, a);
   }
   if (runs == 1) return;
   TraceScope tr("tree_combine", s);
@@ -793,6 +793,7 @@ cs_status launch_tree_attend(const Geo& g, const cs_page_pool& pool, int layer, 
   a.min_tiles = 2 * kWaves;
   a.run_bits = kRunBits;
   a.units = fast_div(even_units(a));
+  a.by_xcd = nr > 1 && room_bytes(g, b) >= 16e6;  // (half of what the L2 caches hold together)
   a.part = (float*)(((uintptr_t)ws + 255) & ~(uintptr_t)255);
   a.part_ml = a.part + 2 * ((size_t)kRuns << a.row_bits) * g.D;
   if (g.dtype == CS_BF16) {

@@ -94,7 +94,7 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, ql = lane & 31, hi = lane >> 5;
 
   Run run;
-  if (!find_run<true>(a0, blockIdx.x, &run)) return;
+  if (!find_run<true, true>(a0, blockIdx.x, &run)) return;
   int64_t left = run.end - run.begin, off = run.off;
   int b = run.b;
 
@@ -505,7 +505,7 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
           *(u32x4*)((uint16_t*)A.t.out + (int64_t)(q.r0 + i) * A.t.o_row + (h * A.t.G + v - i * A.t.G) * A.t.o_head + 8 * (at & 15)) = w;
       }
     } else {
-      const int64_t slot = 2 * (int64_t)blockIdx.x + (t0 == 0);
+      const int64_t slot = 2 * (int64_t)run.w + (t0 == 0);
       float amax = 0.f;
 #pragma unroll
       for (int d = 0; d < 4; ++d)
@@ -628,13 +628,14 @@ void launch_tree_wide(SplitArgs a, void* ws, bool once, hipStream_t s) {
   a.run_bits = kWideRunBits;
   a.min_tiles = 4;
   a.units = fast_div(even_units(a));
+  a.by_xcd = !a.t.mask;
   a.part = (float*)(((uintptr_t)ws + 255) & ~(uintptr_t)255);
   a.part_ml = a.part + 2 * (size_t)kWideRuns * kPartHalfs / 2;
   const int runs = most_runs(a);
   {
     TraceScope tr("tree_attend_wide", s);
-    if (once) CS_LAUNCH(tr, tree_attend_wide<true>, dim3(runs), dim3(kWideThreads), 0, s, a);
-    else CS_LAUNCH(tr, tree_attend_wide<false>, dim3(runs), dim3(kWideThreads), 0, s, a);
+    if (once) CS_LAUNCH(tr, tree_attend_wide<true>, dim3((runs + 7) / 8 * 8), dim3(kWideThreads), 0, s, a);
+    else CS_LAUNCH(tr, tree_attend_wide<false>, dim3((runs + 7) / 8 * 8), dim3(kWideThreads), 0, s, a);
   }
   if (runs == 1) return;
   TraceScope tr("tree_combine_wide", s);
