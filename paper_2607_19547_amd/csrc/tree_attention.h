@@ -216,9 +216,14 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const char* base, in
 }
 
 // Pieces of one query vector's softmax, merged a round at a time: maxima (log2
-// units) and sums, and C elements of the outputs.  A piece whose maximum is
-// -inf saw no key (sum 0) or scores of -inf alone (sum NaN): it counts only
-// where all are like that.
+// units) and sums, and C elements of the outputs.  A piece that saw no key has a
+// maximum of -inf and a sum of 0.  One whose seen scores were all -inf (weight 0
+// beside any other piece) has kOnlyMinusInf, below every finite score, and a sum
+// above 0.  Maxima do not show NaN; a score of NaN is in the sum.  No weight is
+// less than the smallest normal float, which is off by less than that, so
+// a sum or an output that is not finite stays so, wherever the work is cut.
+constexpr float kOnlyMinusInf = -3.40282347e38f, kSmallest = 1.17549435e-38f;
+__device__ __forceinline__ float final_sum(float m, float sum) { return m == kOnlyMinusInf ? __builtin_nanf("") : sum; }
 template <int C>
 struct Merge {
   float m = -INFINITY, sum = 0.f, acc[C] = {};
@@ -227,30 +232,22 @@ struct Merge {
     float mn = m;
 #pragma unroll
     for (int y = 0; y < U; ++y) mn = fmaxf(mn, ml[y].x);
-    if (m != -INFINITY) {
-      const float back = __builtin_amdgcn_exp2f(m - mn);
-      sum *= back;
+    // (two infinities: NaN, and the larger of it and kSmallest is that)
+    const float back = fmaxf(__builtin_amdgcn_exp2f(m - mn), kSmallest);
+    sum *= back;
 #pragma unroll
-      for (int e = 0; e < C; ++e) acc[e] *= back;
-    } else if (mn != -INFINITY) {
-      sum = 0.f;
-    }
+    for (int e = 0; e < C; ++e) acc[e] *= back;
 #pragma unroll
     for (int y = 0; y < U; ++y) {
-      if (ml[y].x == -INFINITY) {
-        if (mn == -INFINITY) sum += ml[y].y;
-        continue;
-      }
-      const float w = __builtin_amdgcn_exp2f(ml[y].x - mn);
-      if (w == 0.f) continue;  // (0 x inf)
+      const float w = fmaxf(__builtin_amdgcn_exp2f(ml[y].x - mn), kSmallest);
       sum = fmaf(w, ml[y].y, sum);
 #pragma unroll
       for (int e = 0; e < C; ++e) acc[e] = fmaf(w, v[y][e], acc[e]);
     }
     m = mn;
   }
-  __device__ __forceinline__ float scale() const { return m == -INFINITY && sum == 0.f ? 0.f : 1.f / sum; }
-  __device__ __forceinline__ float lse() const { return (m + __log2f(sum)) * kLn2; }
+  __device__ __forceinline__ float scale() const { return sum == 0.f ? 0.f : 1.f / final_sum(m, sum); }
+  __device__ __forceinline__ float lse() const { return (m + __log2f(final_sum(m, sum))) * kLn2; }
 };
 
 // Units of a batch whose requests have all as many rows.

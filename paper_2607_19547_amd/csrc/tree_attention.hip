@@ -530,7 +530,10 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const SplitArgs) {
 #pragma unroll
     for (int x = 0; x < NR; ++x) {
       float lt = group_sum(l[x]);
-      if (seen[x] && m[x] == -INFINITY) lt = __builtin_nanf("");  // only scores of -inf were seen
+      if (seen[x] && m[x] == -INFINITY) {
+        m[x] = kOnlyMinusInf;
+        lt += 1.f;
+      }
       if (x > 0 || !first_seg) __syncthreads();  // the previous 16 have been read
       if (lg == 0) {
         s_m[wave][ln] = m[x];

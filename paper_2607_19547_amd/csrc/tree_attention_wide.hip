@@ -475,14 +475,18 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
     const SplitArgs A = args();
     const int vectors = q.n * A.t.G, qv = rt * 256 + 32 * wave + ql;
     float lt = pair_sum(l_run);
-    if (seen && m_use == -INFINITY) lt = __uint_as_float(0x7fc00000u);  // only scores of -inf were seen
+    if (seen && m_use == -INFINITY) {
+      m_use = kOnlyMinusInf;
+      lt += 1.f;
+    }
     if (seg == ntile) {
       // Through LDS, so that the stores write whole lines (stores of the lanes' own
       // 8 bytes, a row each: 61 questions of 388 rows 157 us, so 146).
       // A wavefront has 8 KB of the ring to itself, chunk c of a row at c ^ (row & 15).
       __builtin_amdgcn_s_barrier();  // the last loads of every wavefront have landed
       asm volatile("" ::: "memory");
-      const float inv = m_use == -INFINITY && lt == 0.f ? 0.f : 1.f / lt;
+      lt = final_sum(m_use, lt);
+      const float inv = lt == 0.f ? 0.f : 1.f / lt;
       char* rows = v_at(wave >> 1) + (wave & 1) * 32 * kRow;
       int at = lane;
       asm volatile("" : "+v"(at));  // (places worked out here, not kept through the tiles)
@@ -511,7 +515,7 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
       for (int d = 0; d < 4; ++d)
 #pragma unroll
         for (int r = 0; r < 16; ++r) amax = fmaxf(amax, fabsf(o[d][r]) < INFINITY ? fabsf(o[d][r]) : 0.f);
-      const float inv = lt > 0.f ? 1.f / lt : 1.f;  // (no key seen: zeros; NaN stays)
+      const float inv = lt > 0.f ? 1.f / lt : 1.f;  // (no key seen: zeros; NaN is in the sum)
       amax = pair_max(amax) * inv;
       const int e = amax > 0.f ? min(max(__builtin_amdgcn_frexp_expf(amax), -100), 100) : 0;  // 2^-e stays normal
       const float by = inv * __builtin_ldexpf(1.f, -e);
