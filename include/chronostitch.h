@@ -533,7 +533,10 @@ cs_status qk_norm_rope_append(const cs_geometry* page, const cs_page_pool* pool,
  * accumulation run in float32; in bf16 the probabilities are rounded to bf16
  * for the product with the values.  A row that sees no key gets 0 and -inf.
  * Keys and values that a row does not see do not matter, infinities and NaN
- * included.  Rows of out and lse at row_start[B] and behind it are left as
+ * included.  Of what it sees, a score of NaN or +inf makes the row NaN, lse too, and
+ * so do scores of -inf where there are no others; beside others they are
+ * keys of weight 0.  An element of a value that is infinite or NaN leaves that
+ * element of out infinite or NaN.  Rows of out and lse at row_start[B] and behind it are left as
  * they are.  Results do not depend on timing.
  *
  *   q, out     [n_rows][H_q][D]; out may be q itself (data and strides)

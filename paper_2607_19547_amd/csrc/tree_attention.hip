@@ -93,7 +93,7 @@ __global__ __launch_bounds__(kAnyThreads) void tree_attend_any(const TreeArgs a)
 #pragma unroll
   for (int e = 0; e < 2; ++e)
     if (tid + kAnyThreads * e < a.D) put_elem(op + tid + kAnyThreads * e, any ? acc[e] * inv : 0.f);
-  if (a.lse && tid == 0) a.lse[(int64_t)r * a.Hq + h] = any ? m + logf(l) : -INFINITY;
+  if (a.lse && tid == 0) a.lse[(int64_t)r * a.Hq + h] = !any ? -INFINITY : l == 0.f ? __builtin_nanf("") : m + logf(l);  // (0: only scores of -inf)
 }
 
 // ============================================================== matrix-instruction path

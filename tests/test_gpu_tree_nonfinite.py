@@ -129,7 +129,7 @@ def test_a_score_of_infinity(geo):
     _check(c)
 
 
-@pytest.mark.parametrize("geo", FAST)
+@pytest.mark.parametrize("geo", FAST + ANY)
 @pytest.mark.parametrize("new", [1, 6])
 def test_only_scores_of_minus_infinity(geo, new):
     c = Case(6, [700, 40], [new, new], 16, *geo)
