@@ -530,8 +530,11 @@ cs_status qk_norm_rope_append(const cs_geometry* page, const cs_page_pool* pool,
  * over the keys j that row i of request b sees: every j < cached_len[b], and
  * j = cached_len[b] + w for the rows w < new_len[b] that its mask names (w <= i
  * without a mask).  lse[r][h] = log(sum_j exp(q . K[j] / sqrt(D))).  Softmax and
- * accumulation run in float32; in bf16 the probabilities are rounded to bf16
- * for the product with the values.  A row that sees no key gets 0 and -inf.
+ * accumulation run in float32; in bf16 the probabilities are rounded to bf16 for
+ * the product with the values (the sum in the quotient and lse is of the
+ * unrounded ones), and the parts of a row that several workgroups work on may be
+ * kept in fp16 with an exponent for each row.  Sums of products with values are
+ * divided at the end: |V| x keys up to 2^122 is safe.  A row that sees no key gets 0 and -inf.
  * Keys and values that a row does not see do not matter, infinities and NaN
  * included.  Of what it sees, a score of NaN or +inf makes the row NaN, lse too, and
  * so do scores of -inf where there are no others; beside others they are

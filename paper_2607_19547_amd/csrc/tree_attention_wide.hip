@@ -21,11 +21,11 @@
 //
 // The work is cut as in the kernel for few rows (equal runs of key tiles, one
 // run for each of 256 workgroups, one workgroup per CU).  A piece of a unit
-// leaves its outputs, in the accumulators' own layout, divided by their sum and
-// by 2^e, so that a query vector's largest lies in [0.5, 1), and rounded to fp16:
-// 11 bits relative to that largest element, a quarter of the output's own
-// rounding, for half the bytes of float32 (a launch of 256 pieces leaves 17 MB
-// and the merge reads them: see tree_combine_wide).
+// leaves its outputs, in the accumulators' own layout, divided by 2^e, so that a
+// query vector's largest lies in [2^14, 2^15), and rounded to fp16: 11 bits
+// of every element down to 2^-28 of that largest, an eighth of the output's
+// own rounding, for half the bytes of float32 (a launch of 256 pieces leaves 17
+// MB and the merge reads them: see tree_combine_wide).
 #include <math.h>
 
 #include <type_traits>
@@ -42,6 +42,7 @@ constexpr int kHiLds = 65536;            // LDS bytes below the K ring (the V ri
 constexpr float kRescaleLog2 = 5.f;      // growth of the running maximum before the accumulators are rescaled
 constexpr int kWideRuns = 1 << kWideRunBits;
 constexpr int kPartHalfs = 256 * 128;    // a partial's outputs
+constexpr int kPartExp = 15;             // their largest is below 2^15
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
@@ -515,13 +516,8 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
       for (int d = 0; d < 4; ++d)
 #pragma unroll
         for (int r = 0; r < 16; ++r) amax = fmaxf(amax, fabsf(o[d][r]) < INFINITY ? fabsf(o[d][r]) : 0.f);
-      const float inv = lt > 0.f ? 1.f / lt : 1.f;  // (no key seen: zeros; NaN is in the sum)
-      amax = pair_max(amax) * inv;
-      const int e = amax > 0.f ? min(max(__builtin_amdgcn_frexp_expf(amax), -100), 100) : 0;  // 2^-e stays normal
-      const float by = inv * __builtin_ldexpf(1.f, -e);
-      if (hi == 0)
-        *(float4*)(A.part_ml + (slot * 256 + 32 * wave + ql) * 4) =
-            make_float4(m_use, lt, __builtin_ldexpf(lt > 0.f ? lt : 1.f, e), 0.f);
+      const int e = __builtin_amdgcn_frexp_expf(pair_max(amax)) - kPartExp;  // (of zero: 0)
+      if (hi == 0) *(float4*)(A.part_ml + (slot * 256 + 32 * wave + ql) * 4) = make_float4(m_use, lt, (float)e, 0.f);
       _Float16* pp = (_Float16*)A.part + slot * kPartHalfs + wave * (8 * 512) + lane * 8;
 #pragma unroll
       for (int d = 0; d < 4; ++d)
@@ -529,7 +525,7 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
         for (int r = 0; r < 2; ++r) {
           f16x8 w;
 #pragma unroll
-          for (int x = 0; x < 8; ++x) w[x] = (_Float16)(o[d][8 * r + x] * by);
+          for (int x = 0; x < 8; ++x) w[x] = (_Float16)__builtin_ldexpf(o[d][8 * r + x], -e);
           *(f16x8*)(pp + (2 * d + r) * 512) = w;
         }
     }
@@ -586,7 +582,7 @@ __global__ __launch_bounds__(kStripThreads) void tree_combine_wide(const SplitAr
       for (int y = 0; y < kRound; ++y) {
         ml[y] = x0 + y * step < pieces ? make_float2(st[y].x, st[y].y) : make_float2(-INFINITY, 0.f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[y][e] = (float)v16[y][e] * st[y].z;
+        for (int e = 0; e < 8; ++e) v[y][e] = __builtin_ldexpf((float)v16[y][e], (int)st[y].z);
       }
       mg.add(ml, v);
     }
