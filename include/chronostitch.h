@@ -549,7 +549,7 @@ cs_status qk_norm_rope_append(const cs_geometry* page, const cs_page_pool* pool,
  *              one each
  * Uses batch->cached_len, row_start, block_table and tree_mask.
  * Errors: CS_ERR_INVALID_ARGUMENT, CS_ERR_WORKSPACE_TOO_SMALL,
- * CS_ERR_UNSUPPORTED (grid), CS_ERR_HIP.                                    */
+ * CS_ERR_UNSUPPORTED (grid; max_blocks x P above 2^31 - 65,536), CS_ERR_HIP. */
 cs_status tree_attend_paged_workspace(const cs_geometry* page, const cs_batch* batch, size_t* bytes);
 cs_status tree_attend_paged(const cs_geometry* page, const cs_page_pool* pool, int32_t layer,
                             const cs_batch* batch, const cs_rows* q, const cs_rows* out, float* lse,

@@ -82,6 +82,16 @@ cs_status check_row_count(const Geo& g, const cs_batch& b) {
   return CS_OK;
 }
 
+// Keys are counted in 32 bits: the attention kernels step over a request's keys
+// in tiles and look up pages a few tiles ahead, so the room of a block table
+// (no length goes beyond it) stays that far below 2^31.
+constexpr int64_t kMaxTableTokens = (int64_t(1) << 31) - 65536;
+cs_status check_table(const Geo& g, const cs_batch& b) {
+  if (b.max_blocks > 0 && g.T > kMaxTableTokens / b.max_blocks)
+    return fail(CS_ERR_UNSUPPORTED, "max_blocks x the page's tokens must be at most 2^31 - 65536");
+  return CS_OK;
+}
+
 cs_status check_layer(const Geo& g, int32_t layer) {
   if (layer < 0 || layer >= g.L) return fail(CS_ERR_INVALID_ARGUMENT, "layer out of range");
   return CS_OK;
@@ -159,6 +169,8 @@ cs_status tree_attend_paged_workspace(const cs_geometry* page, const cs_batch* b
   if (!st) st = check_batch(batch);
   if (st) return st;
   if (!bytes) return fail(CS_ERR_INVALID_ARGUMENT, "bytes is NULL");
+  st = check_table(g, *batch);
+  if (st) return st;
   *bytes = batch->n_requests == 0 || batch->n_rows == 0 ? 0 : tree_attend_workspace(g, *batch);
   return CS_OK;
 }
@@ -174,6 +186,7 @@ cs_status tree_attend_paged(const cs_geometry* page, const cs_page_pool* pool, i
   if (st) return st;
   if (batch->n_requests == 0 || batch->n_rows == 0) return CS_OK;
   st = check_row_count(g, *batch);
+  if (!st) st = check_table(g, *batch);
   if (!st) st = check_rows(q, "q");
   if (!st) st = check_rows(out, "out");
   if (!st) st = check_written(g, out, batch->n_rows, g.Hq, "out");

@@ -1,0 +1,23 @@
+"""Limits and contracts of the batch calls that the host decides (no GPU needed)."""
+import ctypes
+
+import pytest
+
+from paper_2607_19547_amd import binding as b
+from tests.test_batch_api import UNS, _attend, _batch, _geo, _r, _says
+
+
+def _workspace(geo, batch):
+    n = ctypes.c_size_t(0)
+    return b.lib().tree_attend_paged_workspace(geo.ref, _r(batch), ctypes.byref(n)), n.value
+
+
+@pytest.mark.parametrize("page,fits", [(64, 33_553_408), (1 << 20, 2047), (1, (1 << 31) - 65536)])
+def test_attention_bounds_the_room_of_a_block_table(built_lib, page, fits):
+    """Key indices, and those a few tiles ahead, stay below 2^31: the largest table that fits, and one block more."""
+    geo = _geo(chunk_start=[0, page])
+    assert fits * page <= (1 << 31) - 65536 < (fits + 1) * page
+    assert _workspace(geo, _batch(max_blocks=fits))[0] == b.CS_OK
+    for call in (lambda x: _workspace(geo, x)[0], lambda x: _attend(geo=geo, batch=x)):
+        assert call(_batch(max_blocks=fits + 1)) == UNS
+        _says("max_blocks")
