@@ -544,9 +544,9 @@ cs_status qk_norm_rope_append(const cs_geometry* page, const cs_page_pool* pool,
  *
  *   q, out     [n_rows][H_q][D]; out may be q itself (data and strides)
  *   lse        DEVICE float32 [n_rows][H_q], or NULL
- *   workspace  DEVICE, >= tree_attend_paged_workspace() of the same geometry
- *              and n_rows; no initial contents needed; calls that overlap need
- *              one each
+ *   workspace  DEVICE, >= tree_attend_paged_workspace() bytes, the same for every
+ *              batch with rows of a geometry (none without); no initial
+ *              contents needed; calls that overlap need one each
  * Uses batch->cached_len, row_start, block_table and tree_mask.
  * Errors: CS_ERR_INVALID_ARGUMENT, CS_ERR_WORKSPACE_TOO_SMALL,
  * CS_ERR_UNSUPPORTED (grid; max_blocks x P above 2^31 - 65,536), CS_ERR_HIP. */

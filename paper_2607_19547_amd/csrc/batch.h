@@ -73,7 +73,7 @@ struct AppendJob {
 };
 cs_status launch_append(const Geo& g, const cs_page_pool& pool, int layer, const cs_batch& b, const AppendJob& job,
                         const double* theta, hipStream_t s, bool check_only);
-size_t tree_attend_workspace(const Geo& g, const cs_batch& b);
+size_t tree_attend_workspace(const Geo& g);
 cs_status launch_tree_attend(const Geo& g, const cs_page_pool& pool, int layer, const cs_batch& b, const cs_rows& q,
                              const cs_rows& out, float* lse, void* ws, hipStream_t s, bool check_only);
 

@@ -171,7 +171,7 @@ cs_status tree_attend_paged_workspace(const cs_geometry* page, const cs_batch* b
   if (!bytes) return fail(CS_ERR_INVALID_ARGUMENT, "bytes is NULL");
   st = check_table(g, *batch);
   if (st) return st;
-  *bytes = batch->n_requests == 0 || batch->n_rows == 0 ? 0 : tree_attend_workspace(g, *batch);
+  *bytes = batch->n_requests == 0 || batch->n_rows == 0 ? 0 : tree_attend_workspace(g);
   return CS_OK;
 }
 
@@ -193,7 +193,7 @@ cs_status tree_attend_paged(const cs_geometry* page, const cs_page_pool* pool, i
   if (st) return st;
   if (out->data == q->data && !same_rows(*q, *out))
     return fail(CS_ERR_INVALID_ARGUMENT, "out in place of q must have q's strides");
-  const size_t need = tree_attend_workspace(g, *batch);
+  const size_t need = tree_attend_workspace(g);
   if (need && (!workspace || workspace_bytes < need))
     return fail(CS_ERR_WORKSPACE_TOO_SMALL,
                 "workspace smaller than tree_attend_paged_workspace() (" + std::to_string(need) + " bytes)");

@@ -694,12 +694,13 @@ static int64_t query_vectors(const Geo& g, const cs_batch& b) { return (int64_t)
 static double room_bytes(const Geo& g, const cs_batch& b) {  // of the keys and values the block tables have room for
   return (double)b.n_requests * b.max_blocks * g.T * g.Hkv * g.D * g.esize * 2;
 }
+static int most_row_groups(const Geo& g) { return g.D > 128 ? 1 : g.D * g.esize > 128 ? 2 : 4; }
 static int row_groups(const Geo& g, const cs_batch& b) {
   const int64_t qv = query_vectors(g, b);
-  if (qv <= 16 || g.D > 128) return 1;
+  if (qv <= 16) return 1;
   const double row_bytes = g.D * g.esize;
   if (room_bytes(g, b) * ((qv + 15) / 16) < 1.6 * (50e6 + 0.3e6 * row_bytes)) return 1;
-  return qv <= 256 || row_bytes > 128 ? 2 : 4;
+  return std::min(most_row_groups(g), qv <= 256 ? 2 : 4);
 }
 
 // Whether the kernel for many rows takes the batch (where its pointers are
@@ -716,11 +717,13 @@ static bool wide(const Geo& g, const cs_batch& b) {
   return wide_type(g) && row_tiles > 1 && room_bytes(g, b) * row_tiles >= 150e6;
 }
 
-size_t tree_attend_workspace(const Geo& g, const cs_batch& b) {
+// The most that any instance of the geometry uses: which one a call takes depends
+// on the batch's sizes and hints, the workspace does not.
+size_t tree_attend_workspace(const Geo& g) {
   if (!has_instance(g)) return 0;
-  const size_t rows = 16 * (size_t)row_groups(g, b);
+  const size_t rows = 16 * (size_t)most_row_groups(g);
   const size_t few = 2 * (size_t)kRuns * rows * (g.D + 2) * sizeof(float) + 512;
-  return wide(g, b) ? std::max(few, tree_wide_workspace()) : few;
+  return wide_type(g) ? std::max(few, tree_wide_workspace()) : few;
 }
 
 template <typename E, int D, int NR, bool ONCE = false>

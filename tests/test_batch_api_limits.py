@@ -21,3 +21,14 @@ def test_attention_bounds_the_room_of_a_block_table(built_lib, page, fits):
     for call in (lambda x: _workspace(geo, x)[0], lambda x: _attend(geo=geo, batch=x)):
         assert call(_batch(max_blocks=fits + 1)) == UNS
         _says("max_blocks")
+
+
+@pytest.mark.parametrize("heads,d,dtype", [((16, 2), 128, "bf16"), ((4, 2), 64, "bf16"), ((4, 1), 256, "bf16"),
+                                           ((8, 2), 128, "f32"), ((3, 1), 64, "f32"), ((4, 4), 16, "f32"), ((2, 1), 80, "bf16")])
+def test_attention_workspace_is_the_geometrys(built_lib, heads, d, dtype):
+    """One size for every batch: no change of its sizes or hints makes a workspace too small."""
+    geo = _geo(n_q_heads=heads[0], n_kv_heads=heads[1], head_dim=d, sections=(d // 2, 0, 0), dtype=dtype)
+    sizes = {_workspace(geo, _batch(n_requests=n, n_rows=rows, max_blocks=blocks, max_rows=most, tree_mask=mask))
+             for n in (1, 64, 4096) for rows in (1, 64, 5000) for blocks in (0, 8, 4096, 200_000) for most in (0, 1, 7, 4000)
+             for mask in (None, 1 << 16)}
+    assert len(sizes) == 1, sizes
