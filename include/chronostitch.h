@@ -468,8 +468,9 @@ enum {
   CS_PLAN_TOO_MANY_ROWS = 8,   /* more than n_rows rows */
   CS_PLAN_MASK_TOO_SMALL = 16, /* a request has more than 64 x mask_words rows */
   CS_PLAN_BAD_PARENT = 32,     /* a parent is neither -1 nor a row before its child: taken for -1 */
-  CS_PLAN_BAD_PAGE = 64        /* a page taken from the free list is outside the pool: used as it is,
-                                  and left out by the other calls */
+  CS_PLAN_BAD_PAGE = 64        /* a page taken from the free list, or a held one that a row of the step
+                                  goes to, is outside the pool: used as it is, and left out by the other
+                                  calls (pages of cached tokens alone are not looked at) */
 };
 
 /* ---------------------------------------------------------------------------

@@ -169,7 +169,9 @@ __global__ __launch_bounds__(kPlanThreads) void batch_plan(const BatchPlanArgs a
   const int b = request_at(r), r0 = s_row[b], i = r - r0;
   const int pos = a.cached[b] + i, blk = a.page.div(pos), h = a.held[b];
   const int page = blk < h ? a.table[(int64_t)b * a.max_blocks + blk] : a.free_pages[s_take[b] + blk - h];
-  a.slot[r] = page >= 0 && page < a.n_pages ? page * P + (pos - blk * P) : -1;
+  const bool in_pool = page >= 0 && page < a.n_pages;
+  a.slot[r] = in_pool ? page * P + (pos - blk * P) : -1;
+  if (!in_pool) atomicOr(a.status, CS_PLAN_BAD_PAGE);
   int depth = i;
   if (a.parent) {
     // ancestors come in descending order, so a mask word is complete when
