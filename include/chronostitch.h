@@ -389,9 +389,10 @@ cs_status selective_attend_scatter_rope_paged(const cs_geometry* g, void* const*
  * A page is a chunk buffer of the *_paged calls, [L][H_kv][P][D] with P tokens,
  * and a pool holds n_pages of them one behind the other, for keys and for
  * values.  The calls below take the geometry of ONE page (n_tokens = P; its
- * chunks are not looked at), and a page can be handed to the *_paged calls as
- * a chunk (k_chunks[c] = k_pages + page x L x H_kv x P x D elements), so a
- * memory is composed where it lies.
+ * chunks, one from 0 to P for instance, are checked as everywhere and not
+ * used), and a page can be handed to the *_paged calls as a chunk (k_chunks[c] =
+ * k_pages + page x L x H_kv x P x D elements), so a memory is composed where it
+ * lies.
  *
  * Token j of request b lies at offset j % P of page block_table[b][j / P].  A
  * request has cached_len[b] tokens behind it and new_len[b] new ones (rows) in
@@ -562,11 +563,15 @@ cs_status tree_attend_paged(const cs_geometry* page, const cs_page_pool* pool, i
  * For every request b and i < n_accepted[b], row accepted[b][i] of the request
  * (its token cached_len[b] + accepted[b][i]) moves to token cached_len[b] + i,
  * keys and values, in the layers [layer_begin, layer_end), and cached_len_out[b]
- * = cached_len[b] + n_accepted[b].  The keys' rotation stays: a row's coordinate
- * is its depth's, which is i.  A path's rows ascend; it ends before the first
- * entry that does not ascend or is not a row of the request (then
- * cached_len_out counts the entries before it).  Every other token is left as
- * it is.  Requests that share a page they write race.
+ * = cached_len[b] + n_accepted[b].  The keys' rotation stays, so accepted[b] is to
+ * be a path: a row whose parent is the cached tokens, then a child of each row
+ * before it (of a question, the first rows).  Then entry i has the coordinate of
+ * depth i, which is the next one.  That it is a path is not checked: other rows
+ * move as they are, with keys turned by the coordinates they were appended
+ * with.  What is checked is that rows ascend: the list ends before the first entry
+ * that does not or is no row of the request (then cached_len_out counts the
+ * entries before it).  Every other token is left as it is.  Requests that share
+ * a page they write race.
  *
  *   accepted        DEVICE int32 [B][max_accept]
  *   n_accepted      DEVICE int32 [B]
