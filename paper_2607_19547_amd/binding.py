@@ -401,6 +401,8 @@ class Batch:
 
     def __init__(self, cached_len, row_start, block_table, slot, coords, tree_mask=None, max_rows=0):
         n, rows = cached_len.shape[0], slot.shape[0]
+        if tree_mask is not None and 0 in tree_mask.shape[1:]:  # (its address would be NULL: no mask)
+            raise ValueError("tree_mask must have at least one word a row")
         self.tensors = (cached_len, row_start, block_table, slot, coords, tree_mask)
         c = self.c = _Batch()
         c.n_requests, c.n_rows, c.max_blocks, c.max_rows = n, rows, block_table.shape[1], int(max_rows)

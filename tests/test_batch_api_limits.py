@@ -32,3 +32,11 @@ def test_attention_workspace_is_the_geometrys(built_lib, heads, d, dtype):
              for n in (1, 64, 4096) for rows in (1, 64, 5000) for blocks in (0, 8, 4096, 200_000) for most in (0, 1, 7, 4000)
              for mask in (None, 1 << 16)}
     assert len(sizes) == 1, sizes
+
+
+def test_binding_refuses_a_mask_without_words(built_lib):
+    """Its address is NULL, which the library takes for a batch without a mask."""
+    torch = pytest.importorskip("torch")
+    i = lambda *s: torch.zeros(s, dtype=torch.int32)
+    with pytest.raises(ValueError, match="word"):
+        b.Batch(i(2), i(3), i(2, 4), i(5), i(5, 3), torch.zeros(5, 0, dtype=torch.int64))
