@@ -16,8 +16,13 @@ LIB_PATH = os.path.join(_PKG, "lib", "libchronostitch.so")
 
 CS_OK, CS_ERR_INVALID_ARGUMENT, CS_ERR_UNSUPPORTED, CS_ERR_WORKSPACE_TOO_SMALL, CS_ERR_HIP = range(5)
 CS_F32, CS_BF16 = 0, 1
-EXPORTS = ("compose_rebase_k", "score_deviation_topk_workspace", "score_deviation_topk",
-           "selective_attend_scatter_workspace", "selective_attend_scatter", "cs_last_error",
+EXPORTS = ("compose_rebase_k", "compose_rebase_k_tokens", "score_deviation_topk_workspace",
+           "score_deviation_topk", "selective_attend_scatter_rope_workspace", "selective_attend_scatter_rope",
+           "selective_attend_scatter_workspace", "selective_attend_scatter", "selective_attend_scatter_noalloc",
+           "compose_rebase_k_paged", "compose_rebase_k_tokens_paged", "compose_load_rebase_k_paged",
+           "score_deviation_topk_paged", "selective_attend_scatter_paged",
+           "selective_attend_scatter_rope_paged", "batch_plan_pages", "qk_norm_rope_append",
+           "tree_attend_paged_workspace", "tree_attend_paged", "tree_commit_paged", "cs_last_error",
            "cs_trace_enable", "cs_trace_only", "cs_trace_collect", "cs_trace_count", "cs_trace_get",
            "cs_trace_reset")
 

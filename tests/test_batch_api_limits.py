@@ -1,5 +1,7 @@
 """Limits and contracts of the batch calls that the host decides (no GPU needed)."""
 import ctypes
+import os
+import re
 
 import pytest
 
@@ -40,3 +42,12 @@ def test_binding_refuses_a_mask_without_words(built_lib):
     i = lambda *s: torch.zeros(s, dtype=torch.int32)
     with pytest.raises(ValueError, match="word"):
         b.Batch(i(2), i(3), i(2, 4), i(5), i(5, 3), torch.zeros(5, 0, dtype=torch.int64))
+
+
+def test_exports_are_the_headers(built_lib):
+    """The binding names every function that the header declares, and the library has each."""
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "chronostitch.h")
+    with open(path) as f:
+        names = re.findall(r"^(?:cs_status|const char\*|int32_t|void) (\w+)\(", f.read(), re.M)
+    assert len(names) > 20 and sorted(b.EXPORTS) == sorted(names)
+    assert all(hasattr(b.lib(), name) for name in names)
