@@ -415,8 +415,9 @@ cs_status selective_attend_scatter_rope_paged(const cs_geometry* g, void* const*
  * reads or writes outside the buffers it was given: a table entry or slot
  * outside the pool is left out (its keys are not seen, its rows not written).
  * max_rows only chooses between kernels: no results but for rounding depend on
- * it.  Calls may overlap where one does not write what another uses.  A batch
- * has at most 4,096 requests, and rows x (H_q + 2 H_kv) below 2^31
+ * it.  Calls may overlap where one does not write what another uses, and what a
+ * call writes must not overlap what it reads but where that is allowed below.
+ * A batch has at most 4,096 requests, and rows x (H_q + 2 H_kv) below 2^31
  * (CS_ERR_UNSUPPORTED beyond); the pool's two buffers are aligned to 16 bytes. */
 typedef struct {
   void* k_pages;               /* DEVICE [n_pages][L][H_kv][P][D] */

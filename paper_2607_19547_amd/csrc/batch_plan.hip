@@ -255,8 +255,8 @@ cs_status launch_batch_plan(const Geo& g, int64_t n_pages, const cs_batch& b, co
 // 16-byte column of one (layer, KV head, K or V) plane and copies it for all
 // entries, kBatchRows loads in flight before their stores, so nothing passes
 // between threads; the rows' places are found once per workgroup, in LDS.  Bound by
-// its chain of loads (lengths, path, table, rows): 4.9 us for one path in 36
-// layers, 5.4 for 48 paths of about four rows (11 MB).
+// its chain of loads (lengths, path, table, rows): 3.9 us for one path in 36
+// layers, 5.5 for 48 paths of about four rows (11 MB).
 constexpr int kCommitThreads = 256;
 constexpr int kPathChunk = 64;
 constexpr int kBatchRows = 8;

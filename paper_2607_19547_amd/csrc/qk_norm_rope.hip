@@ -6,9 +6,10 @@
 // with c, s of coords[axis(i)] * theta_i.  A row's D/2 angles serve all of its
 // heads, so a workgroup takes a few whole rows: its threads make the rows'
 // cos/sin tables in LDS, then groups of lanes take one head each.  Bound by
-// memory: a head is read once and written once (32,762 rows of 16 + 2 x 2 heads of
-// 128 in bf16: 61 us, 5.5 TB/s; 5,172 rows in float32: 23.0 us, 4.6 TB/s; one row:
-// 3.1 us).  Four rows a workgroup make one table entry per thread.
+// memory: a head is read once and written once (the launch, 32,762 rows of 16 + 2 x 2
+// heads of 128 in bf16: 61 us, 5.5 TB/s, with or without a norm; 5,172 rows in
+// float32: 18.9 us, part of them cached; one row: 3.1 us).  Four rows a workgroup
+// make one table entry per thread.
 #include <algorithm>
 
 #include "batch.h"
@@ -92,7 +93,7 @@ __device__ __forceinline__ AppendUnit<E> append_unit(const AppendArgs& a, int r,
 // elements [PV j, PV j + PV) of both halves of the head, 16 bytes each, so a
 // pair's two elements meet in one lane.  ONCE: with the non-temporal hint, for
 // steps whose rows would not stay in the 256 MB cache until they are read (32,762
-// rows of 20 heads, 335 MB: 66.5 -> 62.7 us, 5.3 TB/s; 4,000 rows, 41 MB, cached
+// rows of 20 heads, 335 MB, the whole call: 66.5 -> 62.7 us; 4,000 rows, 41 MB, cached
 // by the calls around it: 10.6 -> 12.8).
 template <typename T, bool ONCE>
 __device__ __forceinline__ T get(const T* p) {
@@ -155,7 +156,8 @@ __global__ __launch_bounds__(kAppendThreads) void qk_norm_rope(const AppendArgs 
   }
 }
 
-// Any even D up to 512, any alignment: one wavefront per head, element by element.
+// Any even D up to 512, any alignment: one wavefront per head, element by element
+// (32,762 rows of 20 heads of 80 in bf16: 197 us, 1.1 TB/s; one row: 8.1 us).
 template <typename E>
 __global__ __launch_bounds__(kAppendThreads) void qk_norm_rope_any(const AppendArgs a) {
   extern __shared__ float2 tab[];

@@ -12,8 +12,9 @@ namespace cs {
 // ============================================================== any geometry
 // One workgroup per (row, query head), keys in blocks of 256: a thread scores
 // one key, then the threads take the head's elements and add up the block's
-// visible values.  Slow (every head reads its keys for itself), right for any
-// even head_dim up to 512, page size and stride.
+// visible values.  Slow (every head reads its keys for itself, and a thread its
+// whole key: 16 / 2 heads of 80 in bf16, one row over 8,211 tokens 2.6 ms, over
+// 1,025 0.18 ms), right for any even head_dim up to 512, page size and stride.
 constexpr int kAnyThreads = 256;
 
 template <typename E>
@@ -98,7 +99,7 @@ __global__ __launch_bounds__(kAnyThreads) void tree_attend_any(const TreeArgs a)
 
 // ============================================================== matrix-instruction path
 // Head dims that fill whole 64-byte pieces of a row (bf16: multiples of 32,
-// float32: of 16, see tree_instance), pages of a multiple of 16 tokens.
+// float32: of 16, see has_instance), pages of a multiple of 16 tokens.
 //
 // A unit is one request, one KV head and a row tile of 16 NR query vectors
 // (its rows x the G query heads that share the KV head).  A wavefront takes a
@@ -682,14 +683,16 @@ static bool has_instance(const Geo& g) {
   return g.D == 16 || g.D == 32 || g.D == 64 || g.D == 128;
 }
 static bool wide_type(const Geo& g) { return g.dtype == CS_BF16 && g.D == 128; }
-// Row tiles of 16, 32 or 64 query vectors.  A larger one reads the keys fewer
-// times, in fewer and longer pieces of work; with rows of more than 128 bytes 64
-// do not fit the registers.  Row tiles of 16 win where they read little in all:
-// measured (us with 16 / 32, 8 query heads a KV head, 6 and 17 rows, 4,000 to
-// 32,000 tokens), the two meet near 200 MB for float32 x 128 (147 MB: 23 / 28, 295
-// MB: 47 / 38), 130 MB for float32 x 64 (74: 16 / 20, 295: 46 / 34) and 90 MB for
-// bf16 x 64 (37: 12 / 14, 147: 24 / 21).  The host knows only the block tables'
-// room, which is seldom filled: the border is put at 1.6 times that.
+// Row tiles of 16, 32 or 64 query vectors.  A larger one reads the keys fewer times, in
+// fewer and longer pieces of work; with rows of more than 128 bytes 64 do not fit the
+// registers (float32 x 128 with 32 spills 12 of them, bf16 x 256 with 16 spills 56).
+// bf16 x 128 has 32 for outputs alone that are not aligned to 16 bytes: the kernel for
+// many rows takes the rest.  Row tiles of 16 win where they read little in all:
+// measured (us with 16 / 32, 8 query heads a KV head, 6 and 17 rows, 4,000 to 32,000
+// tokens), the two meet near 200 MB for float32 x 128 (147 MB: 23 / 28, 295 MB: 47 /
+// 38), 130 MB for float32 x 64 (74: 16 / 20, 295: 46 / 34) and 90 MB for bf16 x 64 (37:
+// 12 / 14, 147: 24 / 21).  The host knows only the block tables' room, which is seldom
+// filled: the border is put at 1.6 times that.
 static int64_t query_vectors(const Geo& g, const cs_batch& b) { return (int64_t)(b.max_rows > 0 ? b.max_rows : b.n_rows) * g.G; }
 static double room_bytes(const Geo& g, const cs_batch& b) {  // of the keys and values the block tables have room for
   return (double)b.n_requests * b.max_blocks * g.T * g.Hkv * g.D * g.esize * 2;
