@@ -220,9 +220,9 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const char* base, in
 // maximum of -inf and a sum of 0.  One whose seen scores were all -inf (weight 0
 // beside any other piece) has kOnlyMinusInf, below every finite score, and a sum
 // above 0.  Maxima do not show NaN; a score of NaN is in the sum.  No weight is
-// less than the smallest normal float, which is off by less than that, so
-// a sum or an output that is not finite stays so, wherever the work is cut.
-constexpr float kOnlyMinusInf = -3.40282347e38f, kSmallest = 1.17549435e-38f;
+// less than the smallest float (which adds at most 2^-21 for any finite output),
+// so a sum or an output that is not finite stays so, wherever the work is cut.
+constexpr float kOnlyMinusInf = -3.40282347e38f, kSmallest = 1.40129846e-45f;  // 2^-149
 __device__ __forceinline__ float final_sum(float m, float sum) { return m == kOnlyMinusInf ? __builtin_nanf("") : sum; }
 template <int C>
 struct Merge {

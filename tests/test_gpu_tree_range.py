@@ -5,6 +5,7 @@ import pytest
 
 from tests.batch_util import Case, attend_tol, f64
 from tests.test_gpu_tree_attention import _run
+from tests.test_gpu_tree_nonfinite import _low_and_high
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -50,4 +51,15 @@ def test_small_values(geo, cached, new):
     """Values of 2^-120 to 2^-119, weights alike (so that the products stay normal floats)."""
     c = Case(2, [cached], [new], 16, *geo, std_q=0.1)
     c.v.copy_((1 + torch.rand(c.v.shape, generator=torch.Generator().manual_seed(0))) * 2.0 ** -120)
+    _check(c)
+
+
+@pytest.mark.parametrize("geo", GEOS[:3])
+@pytest.mark.parametrize("new", [1, 6])
+def test_large_values_far_below_the_others(geo, new):
+    """Values of 2^110 behind scores so far below that they count for nothing (3,000 x 2^110 x e^-128 at most)."""
+    c = _low_and_high(3, new, geo, low=2999)
+    for j in range(2999):
+        page, off = c.table[0][j // 16], j % 16
+        c.v[page, :, :, off] = 2.0 ** 110
     _check(c)
