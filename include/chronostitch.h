@@ -584,6 +584,106 @@ cs_status tree_commit_paged(const cs_geometry* page, const cs_page_pool* pool, i
                             int32_t max_accept, const int32_t* n_accepted, int32_t* cached_len_out,
                             void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Memories held in 4 bits.
+ *
+ * A memory that is composed and repaired can be kept in a packed pool, in 17/32
+ * of a byte an element: pack_pages takes full pages of the pool there,
+ * unpack_rebase_pages brings them back (and to another place on the timeline),
+ * and tree_attend_packed answers from them where they are, the newer tokens in
+ * ordinary pages behind them.
+ *
+ * An element is one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives (e2m1: sign,
+ * two bits of exponent, one of mantissa) times a power of two 2^e that a block
+ * of 32 shares.  Blocks lie along a token's row for keys, and along 32 tokens of
+ * a channel for values.  With amax the largest magnitude in the block, e is the
+ * least from -125 to 125 with amax <= 7 x 2^e (beyond 6 x 2^e saturating costs no more
+ * than rounding costs at 5), elements are rounded to nearest, ties to the even
+ * code.  A block that holds an infinity or a NaN is NaN altogether, and no other
+ * block is.
+ *
+ * A packed page is [L][H_kv] planes of 17/16 x P x D bytes each:
+ *   key codes    [P][D/2]        the even element in the low half of a byte
+ *   key scales   [P/32][D/32][32] e + 127 of block d of each of 32 tokens; 255: NaN
+ *   value codes  [P/8][D][4]     byte w: tokens 2 w (low half) and 2 w + 1 of eight
+ *   value scales [P/32][D]       e + 127 of 32 tokens
+ * P and D are to be multiples of 32 (else CS_ERR_UNSUPPORTED).               */
+typedef struct {
+  void* pages;                 /* DEVICE [n_pages][packed_page_bytes()], aligned to 16 bytes */
+  int64_t n_pages;             /* n_pages x P < 2^31 */
+} cs_packed_pool;
+
+/* Bytes of one packed page of the page geometry. */
+cs_status packed_page_bytes(const cs_geometry* page, size_t* bytes);
+
+/* ---------------------------------------------------------------------------
+ * pack_pages -- pages of the pool into packed pages.
+ *
+ * Page src[i] of the pool goes to page dst[i] of the packed pool, keys and values
+ * of the layers [layer_begin, layer_end), for i < n.  All P tokens of a page are
+ * packed, so a page whose last tokens were never written is not to be packed
+ * (what lies there would take part in its blocks' scales).  Codes and scales are
+ * exact: they depend on the page's contents alone.  An entry whose src or dst is
+ * outside its pool is left out; two entries with one dst leave a mixture.
+ *
+ *   src, dst  DEVICE int32 [n]
+ *   n         >= 0
+ * Errors: CS_ERR_INVALID_ARGUMENT, CS_ERR_UNSUPPORTED (P or D no multiple of 32;
+ * grid), CS_ERR_HIP.                                                        */
+cs_status pack_pages(const cs_geometry* page, const cs_page_pool* pool, const cs_packed_pool* packed,
+                     int32_t layer_begin, int32_t layer_end, const int32_t* src, const int32_t* dst,
+                     int32_t n, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * unpack_rebase_pages -- packed pages back into pages of the pool, re-based on
+ * the way (Eq. 3).
+ *
+ * Page src[i] of the packed pool goes to page dst[i] of the pool; its keys are
+ * turned as compose_rebase_k turns those of a chunk with the offset offsets[i]
+ * (angles in float64, cos and sin in float32, one rounding to the geometry's
+ * type at the end).  With an offset of (0, 0, 0), or without offsets, keys are
+ * the values that the codes stand for, as values always are.  Ranges and entries
+ * outside the pools as for pack_pages.
+ *
+ *   offsets   DEVICE int32 [n][3] (dt, dh, dw), or NULL
+ * Errors: those of pack_pages.                                              */
+cs_status unpack_rebase_pages(const cs_geometry* page, const cs_packed_pool* packed, const cs_page_pool* pool,
+                              int32_t layer_begin, int32_t layer_end, const int32_t* src,
+                              const int32_t* dst, const int32_t* offsets, int32_t n, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * tree_attend_packed -- tree_attend_paged over a memory whose first pages are
+ * packed, or of which a row sees only a span, or both.
+ *
+ * The first packed_blocks[b] entries of request b's block table are pages of the
+ * packed pool, the others pages of the pool.  Packed pages are full of cached
+ * tokens: what goes beyond cached_len[b] / P is not counted.  batch_plan_pages,
+ * qk_norm_rope_append and tree_commit_paged take such a batch as it is: they
+ * touch no page that is full of cached tokens.
+ *
+ * With window > 0 a row sees, of the tokens that it would see in
+ * tree_attend_paged (in their order, itself among them), only the first `sinks`
+ * and the last `window`.  Tokens whose page is outside its pool count, though
+ * they are not seen.  With window = 0 it sees them all, and sinks is not used.
+ *
+ * Everything else is as for tree_attend_paged: out, lse, rows without a key, what
+ * is not finite (a packed block that is NaN makes the keys' scores NaN, or an
+ * element of the values).  In float32 scores and outputs over packed pages are
+ * float32 too: queries and probabilities go into the products as three bf16
+ * terms, which hold all their bits.
+ *
+ *   packed         may be NULL where packed_blocks is
+ *   packed_blocks  DEVICE int32 [B], or NULL: no page is packed
+ *   sinks, window  >= 0
+ *   workspace      DEVICE, >= tree_attend_packed_workspace() bytes, as there
+ * Errors: those of tree_attend_paged; CS_ERR_UNSUPPORTED with packed_blocks where
+ * P or D is no multiple of 32.                                              */
+cs_status tree_attend_packed_workspace(const cs_geometry* page, const cs_batch* batch, size_t* bytes);
+cs_status tree_attend_packed(const cs_geometry* page, const cs_page_pool* pool, const cs_packed_pool* packed,
+                             int32_t layer, const cs_batch* batch, const int32_t* packed_blocks,
+                             int32_t sinks, int32_t window, const cs_rows* q, const cs_rows* out,
+                             float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Thread-local text describing the last non-OK status on this thread. */
 const char* cs_last_error(void);
 

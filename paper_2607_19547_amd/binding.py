@@ -22,7 +22,8 @@ EXPORTS = ("compose_rebase_k", "compose_rebase_k_tokens", "score_deviation_topk_
            "compose_rebase_k_paged", "compose_rebase_k_tokens_paged", "compose_load_rebase_k_paged",
            "score_deviation_topk_paged", "selective_attend_scatter_paged",
            "selective_attend_scatter_rope_paged", "batch_plan_pages", "qk_norm_rope_append",
-           "tree_attend_paged_workspace", "tree_attend_paged", "tree_commit_paged", "cs_last_error",
+           "tree_attend_paged_workspace", "tree_attend_paged", "tree_commit_paged", "packed_page_bytes", "pack_pages",
+           "unpack_rebase_pages", "tree_attend_packed_workspace", "tree_attend_packed", "cs_last_error",
            "cs_trace_enable", "cs_trace_only", "cs_trace_collect", "cs_trace_count", "cs_trace_get",
            "cs_trace_reset")
 
@@ -57,6 +58,10 @@ class Rows(ctypes.Structure):
 
 class _PagePool(ctypes.Structure):
     _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("n_pages", ctypes.c_int64)]
+
+
+class _PackedPool(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p), ("n_pages", ctypes.c_int64)]
 
 
 class _Batch(ctypes.Structure):
@@ -109,6 +114,12 @@ def lib():
         L.tree_attend_paged_workspace.argtypes = [G, B, ctypes.POINTER(sz)]
         L.tree_attend_paged.argtypes = [G, ctypes.POINTER(_PagePool), i32, B, R, R, vp, vp, sz, vp]
         L.tree_commit_paged.argtypes = [G, ctypes.POINTER(_PagePool), i32, i32, B, vp, i32, vp, vp, vp]
+        K = ctypes.POINTER(_PackedPool)
+        L.packed_page_bytes.argtypes = [G, ctypes.POINTER(sz)]
+        L.pack_pages.argtypes = [G, ctypes.POINTER(_PagePool), K, i32, i32, vp, vp, i32, vp]
+        L.unpack_rebase_pages.argtypes = [G, K, ctypes.POINTER(_PagePool), i32, i32, vp, vp, vp, i32, vp]
+        L.tree_attend_packed_workspace.argtypes = [G, B, ctypes.POINTER(sz)]
+        L.tree_attend_packed.argtypes = [G, ctypes.POINTER(_PagePool), K, i32, B, vp, i32, i32, R, R, vp, vp, sz, vp]
         L.cs_last_error.restype = ctypes.c_char_p
         L.cs_trace_enable.argtypes = [i32]
         L.cs_trace_only.argtypes = [ctypes.c_char_p]
@@ -124,7 +135,8 @@ def lib():
                      "compose_load_rebase_k_paged",
                      "selective_attend_scatter_paged", "selective_attend_scatter_rope_paged",
                      "batch_plan_pages", "qk_norm_rope_append", "tree_attend_paged_workspace",
-                     "tree_attend_paged", "tree_commit_paged",
+                     "tree_attend_paged", "tree_commit_paged", "packed_page_bytes", "pack_pages",
+                     "unpack_rebase_pages", "tree_attend_packed_workspace", "tree_attend_packed",
                      "cs_trace_enable", "cs_trace_only", "cs_trace_collect", "cs_trace_get"):
             getattr(L, name).restype = ctypes.c_int
         _lib = L
@@ -362,7 +374,7 @@ def _torch_dtype(dtype, _cache={}):
     if t is None:
         import torch
         _cache.update({CS_F32: torch.float32, CS_BF16: torch.bfloat16, "int32": torch.int32, "int64": torch.int64,
-                       "float32": torch.float32})
+                       "float32": torch.float32, "uint8": torch.uint8})
         t = _cache[dtype]
     return t
 
@@ -522,3 +534,77 @@ def tree_commit_paged(geo, pool, layer_begin, layer_end, batch, accepted, n_acce
                                    accepted.shape[1], _array(n_accepted, "n_accepted", "int32", (n,), batch.device),
                                    _array(cached_len_out, "cached_len_out", "int32", (n,), batch.device, optional=True),
                                    _batch_stream(stream, batch, pool, geo)))
+
+
+# ---------------------------------------------------------------- memories held in 4 bits
+def packed_page_bytes(geo):
+    n = ctypes.c_size_t(0)
+    _check(lib().packed_page_bytes(geo.ref, ctypes.byref(n)))
+    return n.value
+
+
+class PackedPool:
+    """cs_packed_pool: uint8 tensor [n_pages, packed_page_bytes(geo)]."""
+
+    def __init__(self, geo, pages):
+        self.tensors, self.geo = (pages,), geo
+        self.c = _PackedPool()
+        self.c.pages = _array(pages, "pages", "uint8", (None, packed_page_bytes(geo)), None)
+        self.device = pages.get_device()
+        self.c.n_pages = pages.shape[0]
+
+
+def _pages_stream(stream, geo, pool, packed):
+    """The stream, after a look at the pools' geometries and devices (and the current one)."""
+    for p in (pool, packed):
+        if geo is not p.geo and _page_key(geo) != _page_key(p.geo):
+            raise ValueError("the pool's pages are of another geometry")
+    return _batch_stream(stream, pool, packed)
+
+
+def pack_pages(geo, pool, packed, layer_begin, layer_end, src, dst, stream=None):
+    """Pages src of the pool into pages dst of the packed pool (int32 tensors [n]), in layers of a range."""
+    n = src.shape[0]
+    _check(lib().pack_pages(geo.ref, ctypes.byref(pool.c), ctypes.byref(packed.c), int(layer_begin), int(layer_end),
+                            _array(src, "src", "int32", (n,), pool.device), _array(dst, "dst", "int32", (n,), pool.device),
+                            n, _pages_stream(stream, geo, pool, packed)))
+
+
+def unpack_rebase_pages(geo, packed, pool, layer_begin, layer_end, src, dst, offsets=None, stream=None):
+    """Pages src of the packed pool into pages dst of the pool, keys turned by offsets (int32 tensor [n, 3])."""
+    n = src.shape[0]
+    _check(lib().unpack_rebase_pages(geo.ref, ctypes.byref(packed.c), ctypes.byref(pool.c), int(layer_begin),
+                                     int(layer_end), _array(src, "src", "int32", (n,), pool.device),
+                                     _array(dst, "dst", "int32", (n,), pool.device),
+                                     _array(offsets, "offsets", "int32", (n, 3), pool.device, optional=True), n,
+                                     _pages_stream(stream, geo, pool, packed)))
+
+
+def tree_attend_packed_workspace(geo, batch):
+    n = ctypes.c_size_t(0)
+    _check(lib().tree_attend_packed_workspace(geo.ref, ctypes.byref(batch.c), ctypes.byref(n)))
+    return n.value
+
+
+def tree_attend_packed(geo, pool, packed, layer, batch, packed_blocks, q, out, lse=None, workspace=None, sinks=0,
+                       window=0, stream=None):
+    """tree_attend_paged where the first packed_blocks (int32 [B], or None) pages of each request are pages of packed,
+    and where, with window > 0, a row sees the first `sinks` and the last `window` of its tokens."""
+    hq = geo.g.n_q_heads
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    if workspace is not None and (workspace.get_device() != batch.device or not workspace.is_contiguous()):
+        raise ValueError("workspace must be contiguous memory of the batch's device")
+    if lse is not None and lse.shape[0] < batch.c.n_rows:
+        raise ValueError("lse has fewer rows than the batch")
+    if packed is None and packed_blocks is not None:
+        raise ValueError("packed_blocks needs a packed pool")
+    if packed is not None:
+        _batch_stream(0, batch, packed, geo)
+    _check(lib().tree_attend_packed(geo.ref, ctypes.byref(pool.c), None if packed is None else ctypes.byref(packed.c),
+                                    int(layer), ctypes.byref(batch.c),
+                                    _array(packed_blocks, "packed_blocks", "int32", (batch.c.n_requests,), batch.device,
+                                           optional=True), int(sinks), int(window),
+                                    ctypes.byref(_row_arg(q, "q", geo, batch, hq)),
+                                    ctypes.byref(_row_arg(out, "out", geo, batch, hq)),
+                                    _array(lse, "lse", "float32", (None, hq), batch.device, optional=True),
+                                    _ptr(workspace), ws_bytes, _batch_stream(stream, batch, pool, geo)))

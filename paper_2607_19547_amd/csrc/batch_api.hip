@@ -5,6 +5,7 @@
 #include <vector>
 
 #include "batch.h"
+#include "packed_attention.h"
 
 namespace cs {
 
@@ -89,6 +90,37 @@ constexpr int64_t kMaxTableTokens = (int64_t(1) << 31) - 65536;
 cs_status check_table(const Geo& g, const cs_batch& b) {
   if (b.max_blocks > 0 && g.T > kMaxTableTokens / b.max_blocks)
     return fail(CS_ERR_UNSUPPORTED, "max_blocks x the page's tokens must be at most 2^31 - 65536");
+  return CS_OK;
+}
+
+// Pages that can be packed: whole blocks of 32 tokens and of 32 elements.
+cs_status check_packable(const Geo& g) {
+  if (g.T % kBlock || g.D % kBlock)
+    return fail(CS_ERR_UNSUPPORTED, "packed pages need a page's tokens and head_dim to be multiples of 32");
+  if (g.T > (int64_t(1) << 30) / g.D) return fail(CS_ERR_UNSUPPORTED, "a packed page's tokens x head_dim must be at most 2^30");
+  return CS_OK;
+}
+cs_status check_packed(const Geo& g, const cs_packed_pool* p) {
+  if (!p) return fail(CS_ERR_INVALID_ARGUMENT, "packed is NULL");
+  cs_status st = check_n_pages(g, p->n_pages);
+  if (st) return st;
+  if (!p->pages) return fail(CS_ERR_INVALID_ARGUMENT, "the packed pool's pages are NULL");
+  if ((uintptr_t)p->pages & 15) return fail(CS_ERR_INVALID_ARGUMENT, "the packed pool's pages must be aligned to 16 bytes");
+  return CS_OK;
+}
+// What pack_pages and unpack_rebase_pages have in common; *none: nothing to do.
+cs_status check_pages(const cs_geometry* page, Geo* g, const cs_page_pool* pool, const cs_packed_pool* packed, int32_t lb,
+                      int32_t le, const int32_t* src, const int32_t* dst, int32_t n, bool* none) {
+  cs_status st = check_geometry(page, g);
+  if (!st) st = check_packable(*g);
+  if (!st) st = check_pool(*g, pool);
+  if (!st) st = check_packed(*g, packed);
+  if (st) return st;
+  if (lb < 0 || le < lb || le > g->L)
+    return fail(CS_ERR_INVALID_ARGUMENT, "need 0 <= layer_begin <= layer_end <= n_layers");
+  if (n < 0) return fail(CS_ERR_INVALID_ARGUMENT, "n must be >= 0");
+  *none = n == 0 || lb == le;
+  if (n > 0 && (!src || !dst)) return fail(CS_ERR_INVALID_ARGUMENT, "src or dst is NULL");
   return CS_OK;
 }
 
@@ -218,6 +250,86 @@ cs_status tree_commit_paged(const cs_geometry* page, const cs_page_pool* pool, i
     return fail(CS_ERR_INVALID_ARGUMENT, "cached_len_out must not be cached_len");
   return launch_tree_commit(g, *pool, layer_begin, layer_end, *batch, accepted, max_accept, n_accepted, cached_len_out,
                             (hipStream_t)stream, false);
+}
+
+cs_status packed_page_bytes(const cs_geometry* page, size_t* bytes) {
+  Geo g;
+  cs_status st = check_geometry(page, &g);
+  if (!st) st = check_packable(g);
+  if (st) return st;
+  if (!bytes) return fail(CS_ERR_INVALID_ARGUMENT, "bytes is NULL");
+  *bytes = (size_t)packed_view(g, cs_packed_pool{nullptr, 0}).page_bytes;
+  return CS_OK;
+}
+
+cs_status pack_pages(const cs_geometry* page, const cs_page_pool* pool, const cs_packed_pool* packed, int32_t layer_begin,
+                     int32_t layer_end, const int32_t* src, const int32_t* dst, int32_t n, void* stream) {
+  Geo g;
+  bool none;
+  const cs_status st = check_pages(page, &g, pool, packed, layer_begin, layer_end, src, dst, n, &none);
+  if (st || none) return st;
+  return launch_pack(g, *pool, *packed, PagesJob{src, dst, nullptr, n, layer_begin, layer_end}, (hipStream_t)stream, false);
+}
+
+cs_status unpack_rebase_pages(const cs_geometry* page, const cs_packed_pool* packed, const cs_page_pool* pool,
+                              int32_t layer_begin, int32_t layer_end, const int32_t* src, const int32_t* dst,
+                              const int32_t* offsets, int32_t n, void* stream) {
+  Geo g;
+  bool none;
+  cs_status st = check_pages(page, &g, pool, packed, layer_begin, layer_end, src, dst, n, &none);
+  if (st || none) return st;
+  double theta[256];
+  st = thetas(page, g, theta);
+  if (st) return st;
+  return launch_unpack(g, *packed, *pool, PagesJob{src, dst, offsets, n, layer_begin, layer_end}, theta,
+                       (hipStream_t)stream, false);
+}
+
+cs_status tree_attend_packed_workspace(const cs_geometry* page, const cs_batch* batch, size_t* bytes) {
+  Geo g;
+  cs_status st = check_geometry(page, &g);
+  if (!st) st = check_batch(batch);
+  if (st) return st;
+  if (!bytes) return fail(CS_ERR_INVALID_ARGUMENT, "bytes is NULL");
+  st = check_table(g, *batch);
+  if (st) return st;
+  *bytes = batch->n_requests == 0 || batch->n_rows == 0 ? 0 : packed_attend_workspace(g);
+  return CS_OK;
+}
+
+cs_status tree_attend_packed(const cs_geometry* page, const cs_page_pool* pool, const cs_packed_pool* packed,
+                             int32_t layer, const cs_batch* batch, const int32_t* packed_blocks, int32_t sinks,
+                             int32_t window, const cs_rows* q, const cs_rows* out, float* lse, void* workspace,
+                             size_t workspace_bytes, void* stream) {
+  Geo g;
+  cs_status st = check_geometry(page, &g);
+  if (!st) st = check_pool(g, pool);
+  if (!st && packed_blocks) {
+    st = check_packable(g);
+    if (!st) st = check_packed(g, packed);
+  }
+  if (!st) st = check_layer(g, layer);
+  if (!st) st = check_batch(batch);
+  if (st) return st;
+  if (sinks < 0 || window < 0) return fail(CS_ERR_INVALID_ARGUMENT, "sinks and window must be >= 0");
+  if (batch->n_requests == 0 || batch->n_rows == 0) return CS_OK;
+  st = check_row_count(g, *batch);
+  if (!st) st = check_table(g, *batch);
+  if (!st) st = check_rows(q, "q");
+  if (!st) st = check_rows(out, "out");
+  if (!st) st = check_written(g, out, batch->n_rows, g.Hq, "out");
+  if (st) return st;
+  if (out->data == q->data && !same_rows(*q, *out))
+    return fail(CS_ERR_INVALID_ARGUMENT, "out in place of q must have q's strides");
+  const size_t need = packed_attend_workspace(g);
+  if (need && (!workspace || workspace_bytes < need))
+    return fail(CS_ERR_WORKSPACE_TOO_SMALL,
+                "workspace smaller than tree_attend_packed_workspace() (" + std::to_string(need) + " bytes)");
+  // all of it in ordinary pages, all of it seen: the kernels for that
+  if (!packed_blocks && window == 0)
+    return launch_tree_attend(g, *pool, layer, *batch, *q, *out, lse, workspace, (hipStream_t)stream, false);
+  return launch_packed_attend(g, *pool, packed_blocks ? packed : nullptr, layer, *batch, SpanJob{packed_blocks, sinks, window},
+                              *q, *out, lse, workspace, (hipStream_t)stream, false);
 }
 
 }  // extern "C"

@@ -1,0 +1,217 @@
+// Attention of a batch's rows over memories whose first pages are packed, or of
+// which rows see a span (the first `sinks` tokens and the last `window`).
+//
+// The kernel is tree_attend's (tree_attention_few.h) with a loop of its own over
+// the packed tiles before the one over ordinary pages.  A window makes a row
+// tile's work shorter, not its tiles emptier: what lies between the sinks and the
+// first row's window is left out of its count, so runs stay even.
+#include <math.h>
+
+#include <algorithm>
+
+#include "packed_attention.h"
+#include "tree_attention_few.h"
+
+namespace cs {
+
+// ============================================================== any geometry
+// As tree_attend_any: one workgroup per (row, query head), keys in blocks of 256.
+// A packed key's scores and values are decoded one by one.  Slow, right for any
+// even head_dim up to 512, page size and stride.
+constexpr int kAnyThreads = 256;
+
+template <typename E>
+__device__ __forceinline__ float elem(const E* p);
+template <>
+__device__ __forceinline__ float elem<float>(const float* p) { return *p; }
+template <>
+__device__ __forceinline__ float elem<uint16_t>(const uint16_t* p) { return bf16_to_f32(*p); }
+
+template <typename E>
+__global__ __launch_bounds__(kAnyThreads) void packed_attend_any(const MemoryArgs a) {
+  __shared__ float s_q[512], s_p[kAnyThreads], s_red[kAnyThreads / 64];
+  __shared__ int64_t s_at[kAnyThreads];  // where the key lies (packed: its plane), -1 where the row does not see it
+  __shared__ int s_row[kAnyThreads];     // a packed key's row in its page, -1: an ordinary page
+  const TreeArgs& t = a.t;
+  const int r = blockIdx.x, h = blockIdx.y, tid = threadIdx.x, P = t.page.d, D = t.D;
+  if (r >= t.row_start[t.B]) return;
+  int lo = 0, hi = t.B;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (t.row_start[mid] <= r) lo = mid;
+    else hi = mid;
+  }
+  const Request q = load_request(t, lo);
+  const int i = r - q.r0;
+  if (i < 0 || i >= q.n) return;  // (arrays that are no plan's)
+  const int32_t* table = t.table + (int64_t)lo * t.max_blocks;
+  const int64_t lh = (int64_t)t.layer * t.Hkv + h / t.G, plane = lh * P * t.pool.row_bytes;
+  const int packed = a.blocks ? min(max(a.blocks[lo], 0), t.page.div(q.cached)) : 0;
+  const Hidden gone = hidden_keys(a, q, i);
+  const E* qp = (const E*)t.q + r * t.q_row + h * t.q_head;
+  for (int d = tid; d < D; d += kAnyThreads) s_q[d] = elem(qp + d);
+  float m = -INFINITY, l = 0.f, acc[2] = {0.f, 0.f};
+  bool any = false;
+  for (int k0 = 0; k0 < q.len; k0 += kAnyThreads) {
+    if (k0 >= gone.lo && gone.hi - k0 >= kAnyThreads) continue;  // (the whole workgroup)
+    __syncthreads();
+    const int key = k0 + tid;
+    int64_t at = -1;
+    int row = -1;
+    float s = -INFINITY;
+    if (key < q.len && (key < q.cached || sees(t, q, i, key - q.cached)) && !(key >= gone.lo && key < gone.hi)) {
+      const int blk = t.page.div(key), pg = table[blk], off = key - blk * P;
+      if (blk < packed) {
+        if (pg >= 0 && pg < a.packed.n_pages) {
+          at = pg * a.packed.page_bytes + lh * a.packed.plane_bytes();
+          row = off;
+          const unsigned char* p = (const unsigned char*)a.packed.base + at;
+          const unsigned char* sc = p + a.packed.k_scales() + (off >> 5) * D + (off & 31);
+          s = 0.f;
+          for (int d = 0; d < D; ++d)
+            s = fmaf(s_q[d], decode1(p[((int64_t)off * D + d) >> 1] >> (4 * (d & 1)), sc[(d >> 5) * kBlock]), s);
+          s *= t.scale;
+        }
+      } else if (pg >= 0 && pg < t.pool.n_pages) {
+        at = pg * t.pool.page_bytes + plane + (int64_t)off * t.pool.row_bytes;
+        const E* kp = (const E*)(t.pool.k + at);
+        s = 0.f;
+        for (int d = 0; d < D; ++d) s = fmaf(s_q[d], elem(kp + d), s);
+        s *= t.scale;
+      }
+    }
+    float mx = s;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+    if ((tid & 63) == 0) s_red[tid >> 6] = mx;
+    __syncthreads();
+    for (int w = 0; w < kAnyThreads / 64; ++w) mx = fmaxf(mx, s_red[w]);
+    const float m_new = fmaxf(m, mx), ref = m_new == -INFINITY ? 0.f : m_new;
+    const float alpha = expf(m - ref);  // (0 where nothing was seen yet)
+    s_p[tid] = at >= 0 ? expf(s - ref) : 0.f;
+    s_at[tid] = at;
+    s_row[tid] = row;
+    __syncthreads();
+    l *= alpha;
+    acc[0] *= alpha;
+    acc[1] *= alpha;
+    const int cnt = min(kAnyThreads, q.len - k0);
+    for (int x = 0; x < cnt; ++x) {
+      if (s_at[x] < 0) continue;  // an unseen value is not read
+      const float p = s_p[x];
+      const int off = s_row[x];
+      any = true;
+      l += p;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int d = tid + kAnyThreads * e;
+        if (d >= D) break;
+        if (off < 0) {
+          acc[e] = fmaf(p, elem((const E*)(t.pool.v + s_at[x]) + d), acc[e]);
+        } else {
+          const unsigned char* vp = (const unsigned char*)a.packed.base + s_at[x];
+          const uint32_t code = vp[a.packed.v_codes() + ((int64_t)(off >> 3) * D + d) * 4 + ((off & 7) >> 1)] >> (4 * (off & 1));
+          acc[e] = fmaf(p, decode1(code, vp[a.packed.v_scales() + (off >> 5) * D + d]), acc[e]);
+        }
+      }
+    }
+    m = m_new;
+  }
+  E* op = (E*)t.out + r * t.o_row + h * t.o_head;
+  const float inv = any ? 1.f / l : 0.f;
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+    if (tid + kAnyThreads * e < D) put_elem(op + tid + kAnyThreads * e, any ? acc[e] * inv : 0.f);
+  if (t.lse && tid == 0) t.lse[(int64_t)r * t.Hq + h] = !any ? -INFINITY : l == 0.f ? __builtin_nanf("") : m + logf(l);  // (0: only scores of -inf)
+}
+
+// ============================================================== launch
+constexpr int kRunBits = 9, kRuns = 1 << kRunBits;  // workgroups of the attention launch: two for each CU
+
+static bool has_instance(const Geo& g) {
+  if (g.T % 16) return false;
+  if (g.dtype == CS_BF16) return g.D == 32 || g.D == 64 || g.D == 96 || g.D == 128 || g.D == 256;
+  return g.D == 16 || g.D == 32 || g.D == 64 || g.D == 128;
+}
+static int most_row_groups(const Geo& g) { return g.D > 128 || g.D * g.esize > 256 ? 1 : g.D * g.esize > 128 ? 2 : 4; }
+
+size_t packed_attend_workspace(const Geo& g) {
+  const size_t rows = 16 * (size_t)most_row_groups(g);
+  const size_t few = has_instance(g) ? 2 * (size_t)kRuns * rows * (g.D + 2) * sizeof(float) + 512 : 0;
+  return std::max(few, tree_attend_workspace(g));  // (a call without packed pages and window is that one)
+}
+
+template <typename E, int D, int NR, bool ONCE>
+static void run_split(const MemoryArgs& a, hipStream_t s) {
+  const int runs = most_runs(a);
+  {
+    TraceScope tr("packed_attend", s);
+    CS_LAUNCH(tr, (tree_attend<E, D, NR, ONCE, MemoryArgs>), dim3(NR > 1 ? (runs + 7) / 8 * 8 : runs), dim3(kThreads), 0, s, a);
+  }
+  if (runs == 1) return;
+  TraceScope tr("packed_combine", s);
+  CS_LAUNCH(tr, (tree_combine<E, D, (NR > 1), MemoryArgs>), dim3(runs - 1, 2 * NR), dim3(kThreads), 0, s, a);
+}
+template <typename E, int D>
+static void run_split(const MemoryArgs& a, int nr, hipStream_t s) {
+  if constexpr (D * sizeof(E) <= 128)
+    if (nr == 4) return run_split<E, D, 4, false>(a, s);
+  if constexpr (D * sizeof(E) <= 256 && D <= 128)
+    if (nr == 2) return run_split<E, D, 2, false>(a, s);
+  run_split<E, D, 1, false>(a, s);
+}
+
+cs_status launch_packed_attend(const Geo& g, const cs_page_pool& pool, const cs_packed_pool* packed, int layer,
+                               const cs_batch& b, const SpanJob& job, const cs_rows& q, const cs_rows& out, float* lse,
+                               void* ws, hipStream_t s, bool check_only) {
+  MemoryArgs a;
+  TreeArgs& t = a.t;
+  t = tree_args(g, pool, layer, b, q, out, lse);
+  a.packed = packed ? packed_view(g, *packed) : PackedView{};
+  a.blocks = job.blocks;
+  a.sinks = job.sinks;
+  a.window = job.window;
+  a.group = fast_div(g.G);
+  // 16-byte accesses of queries, 4-byte ones of outputs
+  const uint64_t low = (uint64_t)t.q | (uint64_t)((t.q_row | t.q_head) * g.esize);
+  const uint64_t low_o = (uint64_t)t.out | (uint64_t)((t.o_row | t.o_head) * g.esize);
+  if (!has_instance(g) || low % 16 || low_o % 4) {
+    const cs_status st = check_grid(b.n_rows, g.Hq, 1, kAnyThreads, "packed attention");
+    if (st || check_only) return st;
+    TraceScope tr("packed_attend_any", s);
+    const dim3 grid(b.n_rows, g.Hq);
+    if (g.dtype == CS_BF16) CS_LAUNCH(tr, packed_attend_any<uint16_t>, grid, dim3(kAnyThreads), 0, s, a);
+    else CS_LAUNCH(tr, packed_attend_any<float>, grid, dim3(kAnyThreads), 0, s, a);
+    return check_launch("packed attention launch");
+  }
+  if (check_only) return CS_OK;
+  const int64_t qv = (int64_t)(b.max_rows > 0 ? b.max_rows : b.n_rows) * g.G;
+  const int nr = std::min(most_row_groups(g), qv <= 16 ? 1 : qv <= 256 ? 2 : 4);
+  a.row_bits = nr == 1 ? 4 : nr == 2 ? 5 : 6;
+  a.tile_bits = kMemoryTileBits;
+  a.min_tiles = 2 * kWaves;
+  a.run_bits = kRunBits;
+  a.units = fast_div(even_units(a));
+  a.by_xcd = nr > 1;
+  a.part = (float*)(((uintptr_t)ws + 255) & ~(uintptr_t)255);
+  a.part_ml = a.part + 2 * ((size_t)kRuns << a.row_bits) * g.D;
+  if (g.dtype == CS_BF16) {
+    switch (g.D) {
+      case 32: run_split<uint16_t, 32>(a, nr, s); break;
+      case 64: run_split<uint16_t, 64>(a, nr, s); break;
+      case 96: run_split<uint16_t, 96>(a, nr, s); break;
+      case 128: run_split<uint16_t, 128>(a, nr, s); break;
+      default: run_split<uint16_t, 256>(a, nr, s);
+    }
+  } else {
+    switch (g.D) {
+      case 16: run_split<float, 16>(a, nr, s); break;
+      case 32: run_split<float, 32>(a, nr, s); break;
+      case 64: run_split<float, 64>(a, nr, s); break;
+      default: run_split<float, 128>(a, nr, s);
+    }
+  }
+  return check_launch("packed attention launch");
+}
+
+}  // namespace cs

@@ -5,7 +5,7 @@
 
 #include <algorithm>
 
-#include "batch.h"
+#include "packed.h"
 
 namespace cs {
 
@@ -46,6 +46,7 @@ __device__ __forceinline__ bool sees(const TreeArgs& a, const Request& q, int i,
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 struct SplitArgs {
+  static constexpr bool kMemory = false;
   TreeArgs t;
   float* part;      // [2 workgroups][row tile][D] unnormalised partial outputs
   float* part_ml;   // [2 workgroups][row tile][2] their maximum (log2 units) and sum
@@ -57,6 +58,87 @@ struct SplitArgs {
   int by_xcd;       // runs in a row on one XCD
   FastDiv group;    // division by G
 };
+
+// Memories whose first pages are packed, and of which rows see a span
+// (tree_attend_packed).  A key tile of the work has 32 keys: a block of values.
+constexpr int kMemoryTileBits = 5, kMemoryTile = 1 << kMemoryTileBits;
+struct MemoryArgs : SplitArgs {
+  static constexpr bool kMemory = true;
+  PackedView packed;
+  const int32_t* blocks;  // packed pages of every request, or null
+  int sinks, window;      // window 0: every key is seen
+};
+// Key tiles of a request that lie in packed pages: whole pages of cached tokens.
+__device__ __forceinline__ int packed_tiles(const MemoryArgs& a, const Request& q, int b) {
+  if (!a.blocks) return 0;
+  const scalar_ptr n = (scalar_ptr)(uint64_t)a.blocks;
+  const int pages = min(min(max(n[b], 0), a.t.page.div(q.cached)), a.t.max_blocks);
+  return pages * (a.t.page.d >> kMemoryTileBits);
+}
+// What a row tile (rows [i0, i1]) leaves out between the sinks and its rows'
+// windows, in whole key tiles: tile t of its work is key tile t, or t + skip from
+// `sinks` on.  Keys below `low`, and from `high` on, are hidden from no row of it
+// (but for rows among the step's own keys, which are masked in any case).
+struct Span {
+  int sinks, skip, low, high;
+  __device__ __forceinline__ int tile(int t) const { return t >= sinks ? t + skip : t; }
+};
+__device__ __forceinline__ Span span_of(const MemoryArgs& a, const Request& q, int i0, int i1) {
+  Span s = {0, 0, 0x7fffffff, 0};
+  if (!a.window) return s;
+  const int64_t first = (int64_t)q.cached + 1 + (a.t.mask ? 0 : i0) - a.window;  // the first row's window begins here
+  const int64_t last = (int64_t)q.cached + 1 + (a.t.mask ? q.n - 1 : i1) - a.window;
+  s.sinks = (int)(((int64_t)min(a.sinks, q.len) + kMemoryTile - 1) >> kMemoryTileBits);
+  s.skip = max((int)(min(max(first, (int64_t)0), (int64_t)q.len) >> kMemoryTileBits) - s.sinks, 0);
+  s.low = min(a.sinks, q.cached);
+  s.high = (int)min(max(last, (int64_t)0), (int64_t)0x7fffffff);
+  return s;
+}
+// The keys [lo, hi) that the window hides from row i of a request.
+struct Hidden {
+  int lo, hi;
+  // bit w: key k0 + w, of `n` <= 64 keys
+  __device__ __forceinline__ uint64_t bits(int k0, int n) const {
+    const int a = min(max((int64_t)lo - k0, (int64_t)0), (int64_t)n), b = min(max((int64_t)hi - k0, (int64_t)0), (int64_t)n);
+    if (a >= b) return 0;
+    const uint64_t below = b == 64 ? ~0ull : (1ull << b) - 1;
+    return below & ~((1ull << a) - 1);  // (a < b <= 64)
+  }
+};
+__device__ __forceinline__ Hidden hidden_keys(const MemoryArgs& a, const Request& q, int i) {
+  if (!a.window) return {0x7fffffff, 0};
+  int64_t lo = a.sinks, hi = (int64_t)q.cached + i + 1 - a.window;
+  if (a.t.mask) {
+    // the row's visible rows, in order: word by word
+    const unsigned long long* mk = a.t.mask + (int64_t)(q.r0 + i) * a.t.words;
+    const int words = min(a.t.words, (q.n + 63) >> 6);
+    auto word = [&](int w) -> uint64_t {
+      const int n = q.n - 64 * w;
+      return mk[w] & (n >= 64 ? ~0ull : (1ull << n) - 1);
+    };
+    int seen = 0;
+#pragma unroll 1
+    for (int w = 0; w < words; ++w) seen += __popcll(word(w));
+    auto nth = [&](int64_t n) -> int64_t {  // place of the n-th (from 0) of them; behind all keys if there are not so many
+      if (n >= seen) return 0x7fffffff;
+#pragma unroll 1
+      for (int w = 0; w < words; ++w) {
+        uint64_t x = word(w);
+        const int c = __popcll(x);
+        if (n < c) {
+#pragma unroll 1
+          for (; n > 0; --n) x &= x - 1;
+          return 64 * w + __builtin_ctzll(x);
+        }
+        n -= c;
+      }
+      return 0x7fffffff;
+    };
+    if (lo > q.cached) lo = q.cached + nth(lo - q.cached);
+    hi = seen <= a.window ? (int64_t)q.cached + seen - a.window : q.cached + nth(seen - a.window);
+  }
+  return {(int)min(lo, (int64_t)0x7fffffff), (int)min(max(hi, (int64_t)0), (int64_t)0x7fffffff)};
+}
 
 constexpr int kNonTemporal = 2;  // the buffer loads' cache policy bit
 
@@ -82,12 +164,22 @@ struct Units {
 __device__ __forceinline__ int key_tiles(const SplitArgs& a, uint32_t keys) {
   return max((int)((keys + (1 << a.tile_bits) - 1) >> a.tile_bits), 1);
 }
-template <bool PAIRS>
-__device__ __forceinline__ Units unit_sizes(const SplitArgs& a, const Request& q) {
+template <bool PAIRS, class A>
+__device__ __forceinline__ Units unit_sizes(const A& a, const Request& q) {
   Units s;
   s.units = s.nrt = (int)(((int64_t)q.n * a.t.G + (1 << a.row_bits) - 1) >> a.row_bits);
   s.ntile = key_tiles(a, q.len);
-  if (PAIRS && !a.t.mask && s.nrt > 1) {
+  bool whole = true;  // row tiles see everything before them
+  if constexpr (A::kMemory) {
+    if (a.window) {
+      // the sinks, and as many keys as the windows of a row tile's rows (n - 1 more at most) cover
+      const int rows = a.t.mask ? q.n : min(q.n, (int)a.group.div((1 << a.row_bits) - 1) + 2);
+      const int64_t keys = (int64_t)a.window + rows, tiles = (int64_t)min(a.sinks, q.len) + (1 << a.tile_bits) - 1 >> a.tile_bits;
+      s.ntile = (int)min((int64_t)s.ntile, tiles + (keys + (2 << a.tile_bits) >> a.tile_bits));
+      whole = false;
+    }
+  }
+  if (PAIRS && whole && !a.t.mask && s.nrt > 1) {
     // the keys of both: the last rows of p and nrt - 1 - p are, added up, at most n + 2 row tiles' rows
     const int64_t keys = 2 * (int64_t)q.cached + 2 + q.n + a.group.div(2 << a.row_bits);
     const int pair = (int)min((keys + (2 << a.tile_bits) - 2) >> a.tile_bits, 2 * (int64_t)s.ntile), pairs = (s.nrt + 1) >> 1;
@@ -113,8 +205,8 @@ __device__ __forceinline__ int quotient(int64_t x, int64_t d) {
 struct Place {
   int h, rt, t0, n;
 };
-template <bool PAIRS>
-__device__ __forceinline__ Place place_at(const SplitArgs& a, const Request& q, const Units& s, int64_t off) {
+template <bool PAIRS, class A>
+__device__ __forceinline__ Place place_at(const A& a, const Request& q, const Units& s, int64_t off) {
   const int u = uniform(quotient(off, s.ntile));
   Place x;
   x.t0 = uniform((int)(off - (int64_t)u * s.ntile));
@@ -168,8 +260,8 @@ __device__ __forceinline__ int run_of(int x, int64_t total, int64_t len) {
 // the lane whose requests hold the run's first tile, and that lane walks them.
 // Nothing waits for another wavefront.
 // (BLOCK: w is a workgroup's number)
-template <bool PAIRS, bool BLOCK = false>
-__device__ __forceinline__ bool find_run(const SplitArgs& a, int w, Run* run) {
+template <bool PAIRS, bool BLOCK = false, class A>
+__device__ __forceinline__ bool find_run(const A& a, int w, Run* run) {
   if (a.t.B == 1) {
     run->total = request_tiles(a, unit_sizes<PAIRS>(a, load_request_scalar(a.t, 0)));
     const int64_t len = run_length(a, run->total);
@@ -262,6 +354,35 @@ inline int most_runs(const SplitArgs& a) {
   const double tiles = std::max<double>(1, ((double)a.t.max_blocks * a.t.page.d + (1 << a.tile_bits) - 1) / (1 << a.tile_bits));
   const double units = ((double)a.t.n_rows * a.t.G / (1 << a.row_bits) + a.t.B) * a.t.Hkv;
   return (int)std::min<double>(1 << a.run_bits, std::max<double>(a.units.d, ceil(tiles * units / a.min_tiles)));
+}
+
+inline TreeArgs tree_args(const Geo& g, const cs_page_pool& pool, int layer, const cs_batch& b, const cs_rows& q,
+                          const cs_rows& out, float* lse) {
+  TreeArgs t;
+  t.q = q.data;
+  t.out = out.data;
+  t.lse = lse;
+  t.q_row = q.row_stride;
+  t.q_head = q.head_stride;
+  t.o_row = out.row_stride;
+  t.o_head = out.head_stride;
+  t.cached = b.cached_len;
+  t.row_start = b.row_start;
+  t.table = b.block_table;
+  t.mask = (const unsigned long long*)b.tree_mask;
+  t.pool = pool_view(g, pool);
+  t.page = fast_div((int)g.T);
+  t.B = b.n_requests;
+  t.n_rows = b.n_rows;
+  t.max_blocks = b.max_blocks;
+  t.words = b.mask_words;
+  t.layer = layer;
+  t.Hq = g.Hq;
+  t.Hkv = g.Hkv;
+  t.G = g.G;
+  t.D = g.D;
+  t.scale = 1.f / sqrtf((float)g.D);
+  return t;
 }
 
 // The instance for many rows (bf16, head_dim 128): see tree_attention_wide.hip.
