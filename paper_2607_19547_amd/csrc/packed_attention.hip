@@ -135,6 +135,12 @@ static bool has_instance(const Geo& g) {
 }
 static int most_row_groups(const Geo& g) { return g.D > 128 || g.D * g.esize > 256 ? 1 : g.D * g.esize > 128 ? 2 : 4; }
 
+// Whether the kernel for many rows (bf16 x 128) takes the batch.
+static bool wide(const Geo& g, const cs_batch& b) {
+  const int64_t qv = (int64_t)(b.max_rows > 0 ? b.max_rows : b.n_rows) * g.G;
+  return g.dtype == CS_BF16 && g.D == 128 && qv > 64;
+}
+
 size_t packed_attend_workspace(const Geo& g) {
   const size_t rows = 16 * (size_t)most_row_groups(g);
   const size_t few = has_instance(g) ? 2 * (size_t)kRuns * rows * (g.D + 2) * sizeof(float) + 512 : 0;
@@ -185,6 +191,10 @@ cs_status launch_packed_attend(const Geo& g, const cs_page_pool& pool, const cs_
     return check_launch("packed attention launch");
   }
   if (check_only) return CS_OK;
+  if (wide(g, b) && low_o % 16 == 0) {
+    launch_packed_wide(a, ws, false, s);
+    return check_launch("packed attention launch");
+  }
   const int64_t qv = (int64_t)(b.max_rows > 0 ? b.max_rows : b.n_rows) * g.G;
   const int nr = std::min(most_row_groups(g), qv <= 16 ? 1 : qv <= 256 ? 2 : 4);
   a.row_bits = nr == 1 ? 4 : nr == 2 ? 5 : 6;

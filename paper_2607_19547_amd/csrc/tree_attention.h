@@ -60,36 +60,40 @@ struct SplitArgs {
 };
 
 // Memories whose first pages are packed, and of which rows see a span
-// (tree_attend_packed).  A key tile of the work has 32 keys: a block of values.
-constexpr int kMemoryTileBits = 5, kMemoryTile = 1 << kMemoryTileBits;
+// (tree_attend_packed).
 struct MemoryArgs : SplitArgs {
   static constexpr bool kMemory = true;
   PackedView packed;
   const int32_t* blocks;  // packed pages of every request, or null
   int sinks, window;      // window 0: every key is seen
 };
-// Key tiles of a request that lie in packed pages: whole pages of cached tokens.
-__device__ __forceinline__ int packed_tiles(const MemoryArgs& a, const Request& q, int b) {
+// Keys of a request that lie in packed pages: whole pages of cached tokens.
+__device__ __forceinline__ int packed_keys(const MemoryArgs& a, const Request& q, int b) {
   if (!a.blocks) return 0;
   const scalar_ptr n = (scalar_ptr)(uint64_t)a.blocks;
-  const int pages = min(min(max(n[b], 0), a.t.page.div(q.cached)), a.t.max_blocks);
-  return pages * (a.t.page.d >> kMemoryTileBits);
+  return min(min(max(n[b], 0), a.t.page.div(q.cached)), a.t.max_blocks) * a.t.page.d;
+}
+// Whether a key of the table lies in a page of its pool.
+__device__ __forceinline__ bool in_pool(const MemoryArgs& a, int b, int key, int packed) {
+  const int32_t pg = a.t.table[(int64_t)b * a.t.max_blocks + a.t.page.div(key)];
+  return (unsigned)pg < (unsigned)(key < packed ? a.packed.n_pages : a.t.pool.n_pages);
 }
 // What a row tile (rows [i0, i1]) leaves out between the sinks and its rows'
-// windows, in whole key tiles: tile t of its work is key tile t, or t + skip from
-// `sinks` on.  Keys below `low`, and from `high` on, are hidden from no row of it
+// windows, in whole key tiles of 2^BITS: tile t of its work is key tile t, or t + skip
+// from `sinks` on.  Keys below `low`, and from `high` on, are hidden from no row of it
 // (but for rows among the step's own keys, which are masked in any case).
 struct Span {
   int sinks, skip, low, high;
   __device__ __forceinline__ int tile(int t) const { return t >= sinks ? t + skip : t; }
 };
+template <int BITS>
 __device__ __forceinline__ Span span_of(const MemoryArgs& a, const Request& q, int i0, int i1) {
   Span s = {0, 0, 0x7fffffff, 0};
   if (!a.window) return s;
   const int64_t first = (int64_t)q.cached + 1 + (a.t.mask ? 0 : i0) - a.window;  // the first row's window begins here
   const int64_t last = (int64_t)q.cached + 1 + (a.t.mask ? q.n - 1 : i1) - a.window;
-  s.sinks = (int)(((int64_t)min(a.sinks, q.len) + kMemoryTile - 1) >> kMemoryTileBits);
-  s.skip = max((int)(min(max(first, (int64_t)0), (int64_t)q.len) >> kMemoryTileBits) - s.sinks, 0);
+  s.sinks = (int)(((int64_t)min(a.sinks, q.len) + (1 << BITS) - 1) >> BITS);
+  s.skip = max((int)(min(max(first, (int64_t)0), (int64_t)q.len) >> BITS) - s.sinks, 0);
   s.low = min(a.sinks, q.cached);
   s.high = (int)min(max(last, (int64_t)0), (int64_t)0x7fffffff);
   return s;
@@ -393,5 +397,6 @@ size_t tree_wide_workspace();
 // of 65,000 tokens 59 -> 62).
 constexpr double kWideOnceBytes = 64e6;
 void launch_tree_wide(SplitArgs a, void* ws, bool once, hipStream_t s);
+void launch_packed_wide(MemoryArgs a, void* ws, bool once, hipStream_t s);
 
 }  // namespace cs

@@ -46,6 +46,8 @@ __device__ __forceinline__ void put_elem(uint16_t* p, float x) { *p = f32_to_bf1
 // load and a prefix sum).
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
+// Packed pages: a key tile of the work has 32 keys, a block of values.
+constexpr int kMemoryTileBits = 5, kMemoryTile = 1 << kMemoryTileBits;
 // The running maximum may grow by 2^5 before the accumulators are rescaled:
 // probabilities stay far inside the range of both types.
 constexpr float kRescaleLog2 = 5.f;
@@ -175,9 +177,9 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const Args) {
     Span span;
     int t_begin = t0, t_end = min(t0 + seg, (key_end + KT - 1) / KT), packed_end = 0;  // (tiles of KT keys; packed ones, of 32)
     if constexpr (kMemory) {
-      span = span_of(a, q, a.group.div(rt * RT), i_last);
+      span = span_of<kMemoryTileBits>(a, q, a.group.div(rt * RT), i_last);
       const int end = min(t0 + seg, (key_end + kMemoryTile - 1) / kMemoryTile - span.skip);
-      const int packed = packed_tiles(a, q, b);
+      const int packed = packed_keys(a, q, b) >> kMemoryTileBits;
       packed_end = min(end, packed <= span.sinks ? packed : max(packed - span.skip, span.sinks));
       t_begin = max(t0, packed_end) * kSub;
       t_end = end * kSub;

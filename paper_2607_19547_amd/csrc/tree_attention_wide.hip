@@ -39,6 +39,7 @@ constexpr int kWideWaves = 8;
 constexpr int kWideThreads = 64 * kWideWaves;
 constexpr int kRow = 256;                // bytes of a K/V row
 constexpr int kHiLds = 65536;            // LDS bytes below the K ring (the V ring)
+constexpr int kStagedBytes = 1280;       // a wavefront's codes and scales of 8 packed keys
 constexpr float kRescaleLog2 = 5.f;      // growth of the running maximum before the accumulators are rescaled
 constexpr int kWideRuns = 1 << kWideRunBits;
 constexpr int kPartHalfs = 256 * 128;    // a partial's outputs
@@ -58,14 +59,16 @@ __device__ __forceinline__ float pair_sum(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-template <bool ONCE>
-__global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs a0) {
+template <bool ONCE, class Args = SplitArgs>
+__global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const Args a0) {
+  constexpr bool kMemory = Args::kMemory;
   // LDS rows are 256 bytes, a key each, their 16-byte chunks permuted so that
   // the operand reads are free of bank conflicts (K: chunk c of row r at c ^
   // (r & 15); V: at c ^ 4 (r & 3)).  The V ring takes the low 64 KB, where the
   // DS instructions' 16-bit offsets reach; variables are laid out by name.
   __shared__ __attribute__((aligned(1024))) char lo_v0[kKT * kRow], lo_v1[kKT * kRow], lo_v2[kKT * kRow], lo_v3[kKT * kRow];
   __shared__ __attribute__((aligned(1024))) char up_k0[kKT * kRow], up_k1[kKT * kRow], up_k2[kKT * kRow], up_k3[kKT * kRow];
+  __shared__ __attribute__((aligned(1024))) char up_staged[kMemory ? 3 * kWideWaves * kStagedBytes : 4];
   auto kbuf = [&](auto B) -> char* {
     if constexpr (decltype(B)::value == 0) return up_k0;
     else if constexpr (decltype(B)::value == 1) return up_k1;
@@ -85,12 +88,12 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
 
   // The arguments are read again where they are used, so that the tile loop
   // keeps none of them in registers.
-  typedef const __attribute__((address_space(4))) SplitArgs* ArgPtr;
+  typedef const __attribute__((address_space(4))) Args* ArgPtr;
   const ArgPtr argp = (ArgPtr)__builtin_amdgcn_kernarg_segment_ptr();
-  auto args = [&]() -> SplitArgs {
+  auto args = [&]() -> Args {
     ArgPtr p = argp;
     asm volatile("" : "+s"(p));
-    return *(const SplitArgs*)p;
+    return *(const Args*)p;
   };
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, ql = lane & 31, hi = lane >> 5;
 
@@ -125,7 +128,7 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
     Request q;
     int h, rt, t0, ntile;
     {
-      const SplitArgs A = args();
+      const Args A = args();
       if (b >= A.t.B) break;  // (lengths that changed meanwhile)
       q = load_request_scalar(A.t, b);
       const Units units = unit_sizes<true>(A, q);
@@ -148,16 +151,24 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
     const int seg = (int)min(left, (int64_t)(ntile - t0));
     // all_see: keys that every row sees; g_row: the lane's row; w_seen: keys behind it are seen by no row of the wavefront
     int n_kt, key_begin, all_see, g_row, w_seen, bad;
+    Span span;       // (windows)
+    int packed = 0;  // keys in packed pages
     bf16x8 qb[8];
     {
-      const SplitArgs A = args();
+      const Args A = args();
       const int vectors = q.n * A.t.G;
       // rows see no key behind their own without a mask, so later tiles are left out
       const int i_last = A.group.div(min((rt + 1) * 256, vectors) - 1);
       const int key_end = A.t.mask ? q.len : min(q.len, q.cached + i_last + 1);
       all_see = min(A.t.mask ? q.cached : q.cached + A.group.div(rt * 256) + 1, q.len);
       key_begin = t0 * kKT;
-      n_kt = max(min(t0 + seg, (key_end + kKT - 1) / kKT) - t0, 0);
+      if constexpr (kMemory) {
+        span = span_of<kWideTileBits>(A, q, A.group.div(rt * 256), i_last);
+        packed = packed_keys(A, q, b);
+        n_kt = max(min(t0 + seg, (key_end + kKT - 1) / kKT - span.skip) - t0, 0);
+      } else {
+        n_kt = max(min(t0 + seg, (key_end + kKT - 1) / kKT) - t0, 0);
+      }
       const int v0 = rt * 256 + 32 * wave;
       const int qv = min(v0 + ql, vectors - 1);
       g_row = A.group.div(qv);
@@ -174,7 +185,7 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
     int64_t page_bytes;
     int n_pages;
     {
-      const SplitArgs A = args();
+      const Args A = args();
       page = A.t.page;
       table = (scalar_ptr)(uint64_t)(A.t.table + (int64_t)b * A.t.max_blocks);
       const int64_t plane = ((int64_t)A.t.layer * A.t.Hkv + h) * page.d * kRow;
@@ -184,11 +195,65 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
       n_pages = A.t.pool.n_pages;
     }
     const int last_key = q.len - 1, key_wave = key_begin + 8 * wave;
+    auto key_of = [&](int i) {  // the first of this wavefront's keys of tile i
+      if constexpr (kMemory) return span.tile(t0 + i) * kKT + 8 * wave;
+      else return key_wave + i * kKT;
+    };
     auto find_page = [&](int i) {
-      if (last_key >= 0) page_next = table[page.div(min(key_wave + i * kKT, last_key))];
+      if (last_key >= 0) page_next = table[page.div(min(key_of(i), last_key))];
+    };
+    // Packed keys: a wavefront's codes and scales come by buffer-to-LDS loads, two
+    // tiles ahead of their place in the ring, and go there from its staging place
+    // as bf16, laid out as loads of rows leave them (tile i + 2 in step i).  Eight
+    // lanes have a key, 16 elements each; of the values a lane has two channels of
+    // all eight.
+    const char* p_plane = nullptr;
+    int64_t packed_bytes = 0;
+    int n_packed = 0, page_codes = 0;
+    if constexpr (kMemory) {
+      const Args A = args();
+      p_plane = A.packed.base + ((int64_t)A.t.layer * A.t.Hkv + h) * A.packed.plane_bytes();
+      packed_bytes = A.packed.page_bytes;
+      n_packed = A.packed.n_pages;
+    }
+    auto is_packed = [&](int i) { return kMemory && i < n_kt && key_of(i) < packed; };
+    auto staged = [&](int i) -> char* { return up_staged + (i % 3 * kWideWaves + wave) * kStagedBytes; };
+    auto find_codes = [&](int i) {
+      if (packed > 0) page_codes = table[page.div(min(key_of(i), packed - 1))];
+    };
+    auto load_codes = [&](int i) {
+      const PackedView pv = {nullptr, 0, 0, page.d, 128};
+      const int key = key_of(i), in_page = key - page.div(key) * page.d, c = in_page * 64, sc = (in_page >> 5) * 128;
+      const char* p = p_plane + page_codes * packed_bytes;
+      const bool ok = (unsigned)page_codes < (unsigned)n_packed;  // (no bytes: no address is used)
+      const auto rc = rows_rsrc(p + c, ok ? pv.plane_bytes() - c : 0), rs = rows_rsrc(p + sc, ok ? pv.plane_bytes() - sc : 0);
+      int x = lane;
+      asm volatile("" : "+v"(x));  // (places worked out here, not kept through the tiles)
+      // 512 bytes of key codes, 512 of value codes; 4 x 8 bytes of key scales, 128 of value scales
+      const int at = x < 32 ? 16 * x : pv.v_codes() - 512 + 16 * x;
+      const int as = x < 8 ? pv.k_scales() + (in_page & 31) + 16 * x - 12 * (x & 1) : pv.v_scales() - 32 + 4 * x;
+      char* to = staged(i);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rc, (lds_void*)to, 16, at, 0, 0, ONCE ? kNonTemporal : 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(to + 1024), 4, as, 0, 0, ONCE ? kNonTemporal : 0);
+      find_codes(i + 1);
+    };
+    auto put_codes = [&](int i, char* Kd, char* Vd) {
+      int x = lane;
+      asm volatile("" : "+v"(x));
+      const char* from = staged(i);
+      const int r = 8 * wave + (x >> 3), c = 2 * (x & 7);
+      const u32x2 kc = *(const u32x2*)(from + 8 * x), vc = *(const u32x2*)(from + 512 + 8 * x);
+      const float ks = scale_of<0>(*(const uint8_t*)(from + 1024 + 4 * (x & 6) + (x >> 3)));
+      const uint32_t vs = *(const uint16_t*)(from + 1056 + 2 * x);
+      *(bf16x8*)(Kd + r * kRow + 16 * (c ^ (r & 15))) = decode8(kc[0], ks);
+      *(bf16x8*)(Kd + r * kRow + 16 * ((c + 1) ^ (r & 15))) = decode8(kc[1], ks);
+      const bf16x8 v0 = decode8(vc[0], scale_of<0>(vs)), v1 = decode8(vc[1], scale_of<1>(vs));
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        *(bf16x2*)(Vd + (8 * wave + j) * kRow + 16 * ((x >> 2) ^ ((j & 3) << 2)) + 4 * (x & 3)) = bf16x2{v0[j], v1[j]};
     };
     auto fetch = [&](int i, char* Kd, char* Vd) {
-      const int key = key_wave + i * kKT;
+      const int key = key_of(i);
       const bool ok = i < n_kt && key <= last_key && (unsigned)page_next < (unsigned)n_pages;
       const int64_t at = page_next * page_bytes + (int64_t)(key - page.div(key) * page.d) * kRow;
       const int bytes = ok ? min(last_key + 1 - key, 8) * kRow : 0;  // (no bytes: no address is used)
@@ -201,11 +266,39 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
       }
       find_page(i + 1);
     };
+    // Step i's part of the ring's filling: tile i + 3 of ordinary pages is fetched;
+    // packed, tile i + 2 is put there and tile i + 4 loaded.
+    auto fill = [&](int i, char* K2, char* V2, char* K3, char* V3) {
+      if constexpr (kMemory) {
+        if (is_packed(i + 2)) {
+          // (behind its loads are those of tile i + 3, if any)
+          if (is_packed(i + 3)) asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
+          else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+          put_codes(i + 2, K2, V2);
+          if (is_packed(i + 4)) load_codes(i + 4);
+        }
+        if (is_packed(i + 3)) {
+          find_page(i + 4);
+          return;
+        }
+      }
+      fetch(i + 3, K3, V3);
+    };
+    if constexpr (kMemory) {
+      find_codes(0);
+#pragma unroll 1
+      for (int i = 0; i < 3; ++i)
+        if (is_packed(i)) load_codes(i);
+    }
+    auto fetch_first = [&](int i, char* Kd, char* Vd) {
+      if (is_packed(i)) find_page(i + 1);
+      else fetch(i, Kd, Vd);
+    };
     find_page(0);
-    fetch(0, up_k0, lo_v0);
-    fetch(1, up_k1, lo_v1);
+    fetch_first(0, up_k0, lo_v0);
+    fetch_first(1, up_k1, lo_v1);
     {
-      const SplitArgs A = args();
+      const Args A = args();
       const int qv = min(rt * 256 + 32 * wave + ql, q.n * A.t.G - 1);
       const uint16_t* qp = (const uint16_t*)A.t.q + (int64_t)(q.r0 + g_row) * A.t.q_row +
                            (h * A.t.G + qv - g_row * A.t.G) * A.t.q_head + 8 * hi;
@@ -213,13 +306,26 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
       for (int s = 0; s < 8; ++s) qb[s] = *(const bf16x8*)(qp + 16 * s);
       // pages of this piece that are none of the pool
       bad = 0;
-      if (n_kt > 0) {
+      if constexpr (kMemory) {
+        for (int x = tid; x < 4 * n_kt; x += kWideThreads) {  // (16 keys are of one page)
+          const int key = span.tile(t0 + (x >> 2)) * kKT + 16 * (x & 3);
+          bad |= key < q.len && !in_pool(A, b, key, packed);
+        }
+      } else if (n_kt > 0) {
         const int p0 = A.t.page.div(key_begin), p1 = A.t.page.div(min(key_begin + n_kt * kKT, q.len) - 1);
         const int32_t* tb = A.t.table + (int64_t)b * A.t.max_blocks;
         for (int x = p0 + tid; x <= p1; x += kWideThreads) bad |= tb[x] < 0 || tb[x] >= A.t.pool.n_pages;
       }
     }
-    fetch(2, up_k2, lo_v2);
+    fetch_first(2, up_k2, lo_v2);
+    if constexpr (kMemory) {
+      if (is_packed(0)) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        put_codes(0, up_k0, lo_v0);
+        if (is_packed(1)) put_codes(1, up_k1, lo_v1);
+        if (is_packed(3)) load_codes(3);
+      }
+    }
     bad = __syncthreads_or(bad);
 
     f32x16 o[4];
@@ -251,7 +357,7 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
     // the pool: the keys that the lane's row does not see get -inf.
     // Accumulator register r of block y holds key kt + 32 y + 8 (r / 4) + 4 hi + r % 4.
     auto visible = [&](int kt) -> uint64_t {  // bit 32 y + 8 (r / 4) + r % 4 belongs to register r of block y
-      const SplitArgs A = args();
+      const Args A = args();
       uint64_t vis;
       {
         const int w0 = kt - q.cached, w = max(w0, 0);
@@ -268,7 +374,12 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
         vis = w0 <= -64 ? ~0ull : w0 < 0 ? bits << -w0 | ((1ull << -w0) - 1) : bits;
         const int n = q.len - kt;
         vis &= n >= 64 ? ~0ull : (1ull << n) - 1;
-        if (bad) {
+        if constexpr (kMemory) {
+          if (A.window) vis &= ~hidden_keys(A, q, g_row).bits(kt, 64);
+          if (bad)
+            for (int y = 0; y < 4; ++y)
+              if (!in_pool(A, b, min(kt + 16 * y, q.len - 1), packed)) vis &= ~(0xffffull << (16 * y));
+        } else if (bad) {
           const scalar_ptr tb = (scalar_ptr)(uint64_t)(A.t.table + (int64_t)b * A.t.max_blocks);
           for (int y = 0; y < 4; ++y) {
             const int pg = tb[A.t.page.div(min(kt + 16 * y, q.len - 1))];
@@ -411,69 +522,94 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
     // Tile i is in ring slot C, tile i + 1 in N; tile i + 3 goes to S (read last
     // in step i - 1).  Each wavefront waits for its part of tile i + 2 (all but
     // its four newest loads) before the barrier.
+    // (Packed keys: its writes of tile i + 3, too.)
+    auto landed = [&]() {
+      if constexpr (kMemory) asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)" ::: "memory");
+      else asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      if constexpr (kMemory) asm volatile("" ::: "memory");
+    };
+    auto next = [](auto B) { return std::integral_constant<int, (decltype(B)::value + 1) & 3>{}; };
     auto step = [&](auto C, auto N, auto S, int i, f32x16& c0, f32x16& c1, f32x16& n0, f32x16& n1) {
-      fetch(i + 3, kbuf(S), vbuf(S));
+      fill(i, kbuf(next(N)), vbuf(next(N)), kbuf(S), vbuf(S));
       if (w_seen >= 0) {
         qk_head(kbuf(N), n0, n1);
         tile_max(c0, c1);
         exp_pv_qk(vbuf(C), kbuf(N), c0, c1, n0, n1);
       }
-      asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
-      __builtin_amdgcn_s_barrier();
+      landed();
     };
     // First the tiles that every row sees whole, their ring slots known to the
     // compiler, a tile's scores computed a step ahead; then, in a plain loop, the
     // few with the step's own rows.
-    const int n_clear = bad ? 0 : min(max(all_see / kKT - t0, 0), n_kt);
-    f32x16 sa0, sa1, sb0, sb1;
-    asm volatile("s_waitcnt vmcnt(4)" ::: "memory");  // tiles 0 and 1 and the queries have landed
-    __builtin_amdgcn_s_barrier();
-    if (n_clear > 0) qk(up_k0, sa0, sa1);
-    for (int i = 0; i < n_clear; i += 4) {
-      step(I0{}, I1{}, I3{}, i, sa0, sa1, sb0, sb1);
-      if (i + 1 >= n_clear) break;
-      step(I1{}, I2{}, I0{}, i + 1, sb0, sb1, sa0, sa1);
-      if (i + 2 >= n_clear) break;
-      step(I2{}, I3{}, I1{}, i + 2, sa0, sa1, sb0, sb1);
-      if (i + 3 >= n_clear) break;
-      step(I3{}, I0{}, I2{}, i + 3, sb0, sb1, sa0, sa1);
+    // With windows there are masked ones before them, too, as many as the ring has
+    // slots or a multiple of that.
+    int n_clear = 0, clear0 = 0;  // tiles [clear0, n_clear)
+    if constexpr (kMemory) {
+      auto place = [&](int keys) {  // of the first tile that begins at `keys` or behind it, among the unit's
+        const int x = (keys + kKT - 1) / kKT;
+        return x <= span.sinks ? x : max(x - span.skip, span.sinks);
+      };
+      if (!bad) {
+        if (span.high > span.low) clear0 = min((max(place(span.high) - t0, 0) + 3) & ~3, n_kt);
+        n_clear = min(max(place(all_see / kKT * kKT) - t0, clear0), n_kt);
+      }
+    } else {
+      n_clear = bad ? 0 : min(max(all_see / kKT - t0, 0), n_kt);
     }
-    seen = n_clear > 0;
+    f32x16 sa0, sa1, sb0, sb1;
+    landed();  // tiles 0 and 1 and the queries
     auto k_at = [&](int x) -> char* { return x & 2 ? (x & 1 ? up_k3 : up_k2) : (x & 1 ? up_k1 : up_k0); };
     auto v_at = [&](int x) -> char* { return x & 2 ? (x & 1 ? lo_v3 : lo_v2) : (x & 1 ? lo_v1 : lo_v0); };
 #pragma unroll 1
-    for (int i = n_clear; i < n_kt; ++i) {
-      const int kt = key_begin + i * kKT;
-      fetch(i + 3, k_at(i + 3), v_at(i + 3));
-      char* V = v_at(i);
-      if (kt <= w_seen) {
-        qk(k_at(i), sa0, sa1);
-        mask(kt, sa0, sa1);
-        tile_max(sa0, sa1);
-      }
-      not_finite(V, kt);  // (has barriers: every wavefront)
-      if (kt <= w_seen) {
-        const float nm = m_use == -INFINITY ? 0.f : -m_use;
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-          bf16x8 pb;
-#pragma unroll
-          for (int x = 0; x < 8; ++x) {
-            const float p = __builtin_amdgcn_exp2f(fmaf((ks < 2 ? sa0 : sa1)[8 * (ks & 1) + x], sc, nm));
-            l_run += p;
-            pb[x] = (__bf16)p;
-          }
-#pragma unroll
-          for (int d = 0; d < 4; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(V, ks, d), pb, o[d], 0, 0, 0);
+    for (int pass = kMemory ? 0 : 1; pass < 2; ++pass) {
+      if (pass) {
+        if (n_clear > clear0) qk(up_k0, sa0, sa1);
+        for (int i = clear0; i < n_clear; i += 4) {
+          step(I0{}, I1{}, I3{}, i, sa0, sa1, sb0, sb1);
+          if (i + 1 >= n_clear) break;
+          step(I1{}, I2{}, I0{}, i + 1, sb0, sb1, sa0, sa1);
+          if (i + 2 >= n_clear) break;
+          step(I2{}, I3{}, I1{}, i + 2, sa0, sa1, sb0, sb1);
+          if (i + 3 >= n_clear) break;
+          step(I3{}, I0{}, I2{}, i + 3, sb0, sb1, sa0, sa1);
         }
+        if constexpr (kMemory) seen = seen || n_clear > clear0;
+        else seen = n_clear > 0;
       }
-      asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
-      __builtin_amdgcn_s_barrier();
+#pragma unroll 1
+      for (int i = pass ? n_clear : 0; i < (pass ? n_kt : clear0); ++i) {
+        const int kt = kMemory ? span.tile(t0 + i) * kKT : key_begin + i * kKT;
+        fill(i, k_at(i + 2), v_at(i + 2), k_at(i + 3), v_at(i + 3));
+        char* V = v_at(i);
+        if (kt <= w_seen) {
+          qk(k_at(i), sa0, sa1);
+          mask(kt, sa0, sa1);
+          tile_max(sa0, sa1);
+        }
+        not_finite(V, kt);  // (has barriers: every wavefront)
+        if (kt <= w_seen) {
+          const float nm = m_use == -INFINITY ? 0.f : -m_use;
+#pragma unroll
+          for (int ks = 0; ks < 4; ++ks) {
+            bf16x8 pb;
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+              const float p = __builtin_amdgcn_exp2f(fmaf((ks < 2 ? sa0 : sa1)[8 * (ks & 1) + x], sc, nm));
+              l_run += p;
+              pb[x] = (__bf16)p;
+            }
+#pragma unroll
+            for (int d = 0; d < 4; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(V, ks, d), pb, o[d], 0, 0, 0);
+          }
+        }
+        landed();
+      }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 
     // Results: accumulator register r of block d holds dim 32d + 8(r/4) + 4hi + r%4.
-    const SplitArgs A = args();
+    const Args A = args();
     const int vectors = q.n * A.t.G, qv = rt * 256 + 32 * wave + ql;
     float lt = pair_sum(l_run);
     if (seen && m_use == -INFINITY) {
@@ -545,7 +681,8 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const SplitArgs
 constexpr int kStripThreads = 256;
 constexpr int kStripShare = 4;
 constexpr int kRound = 8;
-__global__ __launch_bounds__(kStripThreads) void tree_combine_wide(const SplitArgs a) {
+template <class Args = SplitArgs>
+__global__ __launch_bounds__(kStripThreads) void tree_combine_wide(const Args a) {
   __shared__ float s_acc[4][8][64], s_m[4][64], s_l[4][64];
   const TreeArgs& t = a.t;
   const int w1 = blockIdx.x + 1;
@@ -622,7 +759,8 @@ __global__ __launch_bounds__(kStripThreads) void tree_combine_wide(const SplitAr
 
 size_t tree_wide_workspace() { return 2 * (size_t)kWideRuns * (kPartHalfs * sizeof(_Float16) + 4 * 256 * sizeof(float)) + 512; }
 
-void launch_tree_wide(SplitArgs a, void* ws, bool once, hipStream_t s) {
+template <class Args>
+static void run_wide(Args a, void* ws, bool once, const char* name, const char* combine_name, hipStream_t s) {
   a.row_bits = kWideRowBits;
   a.tile_bits = kWideTileBits;
   a.run_bits = kWideRunBits;
@@ -633,13 +771,19 @@ void launch_tree_wide(SplitArgs a, void* ws, bool once, hipStream_t s) {
   a.part_ml = a.part + 2 * (size_t)kWideRuns * kPartHalfs / 2;
   const int runs = most_runs(a);
   {
-    TraceScope tr("tree_attend_wide", s);
-    if (once) CS_LAUNCH(tr, tree_attend_wide<true>, dim3((runs + 7) / 8 * 8), dim3(kWideThreads), 0, s, a);
-    else CS_LAUNCH(tr, tree_attend_wide<false>, dim3((runs + 7) / 8 * 8), dim3(kWideThreads), 0, s, a);
+    TraceScope tr(name, s);
+    if (once) CS_LAUNCH(tr, (tree_attend_wide<true, Args>), dim3((runs + 7) / 8 * 8), dim3(kWideThreads), 0, s, a);
+    else CS_LAUNCH(tr, (tree_attend_wide<false, Args>), dim3((runs + 7) / 8 * 8), dim3(kWideThreads), 0, s, a);
   }
   if (runs == 1) return;
-  TraceScope tr("tree_combine_wide", s);
-  CS_LAUNCH(tr, tree_combine_wide, dim3(runs - 1, kStripShare), dim3(kStripThreads), 0, s, a);
+  TraceScope tr(combine_name, s);
+  CS_LAUNCH(tr, (tree_combine_wide<Args>), dim3(runs - 1, kStripShare), dim3(kStripThreads), 0, s, a);
+}
+void launch_tree_wide(SplitArgs a, void* ws, bool once, hipStream_t s) {
+  run_wide(a, ws, once, "tree_attend_wide", "tree_combine_wide", s);
+}
+void launch_packed_wide(MemoryArgs a, void* ws, bool once, hipStream_t s) {
+  run_wide(a, ws, once, "packed_attend_wide", "packed_combine_wide", s);
 }
 
 }  // namespace cs

@@ -59,9 +59,15 @@ class PackedCase(Case):
 def tol(out, lse, spread, dtype):
     """attend_tol's bounds; in float32 a score and an output are sums of three times as many products (three bf16
     terms of a query or a probability, each product exact), so three times the terms of those sums."""
-    if dtype == "bf16":
-        return attend_tol(out, lse, spread, dtype)
     d = out.shape[-1]
+    if dtype == "bf16":
+        t, t_lse = attend_tol(out, lse, spread, dtype)
+        if d == 128:
+            # Many rows leave their pieces in fp16, scaled so that a row's largest element lies in [2^14, 2^15): half a
+            # step is 2^-11 of an element, and at most 2^-25 where elements are so small that steps are even, which is
+            # 2^-39 of the largest.  Weighted like the pieces' outputs, these add up to as much of sum p |V|.
+            t = t + 2.0 ** -11 * spread[..., :d] + 2.0 ** -39 * spread[..., :d].max(-1, keepdims=True)
+        return t, t_lse
     rel = (3 * d + 16) * 2.0 ** -24 * (1 + spread[..., d]) + (3 * spread[..., d + 1] + 64) * 2.0 ** -24
     with np.errstate(invalid="ignore"):
         t = spread[..., :d] * (2 * rel)[..., None] * (1 + 2.0 ** -24) + 2.0 ** -24 * np.abs(out) + 1e-30
