@@ -191,6 +191,7 @@ cs_status launch_packed_attend(const Geo& g, const cs_page_pool& pool, const cs_
     return check_launch("packed attention launch");
   }
   if (check_only) return CS_OK;
+  a.paged_bits = a.unit_tiles = 0;
   if (wide(g, b) && low_o % 16 == 0) {
     launch_packed_wide(a, ws, false, s);
     return check_launch("packed attention launch");
@@ -198,7 +199,9 @@ cs_status launch_packed_attend(const Geo& g, const cs_page_pool& pool, const cs_
   const int64_t qv = (int64_t)(b.max_rows > 0 ? b.max_rows : b.n_rows) * g.G;
   const int nr = std::min(most_row_groups(g), qv <= 16 ? 1 : qv <= 256 ? 2 : 4);
   a.row_bits = nr == 1 ? 4 : nr == 2 ? 5 : 6;
-  a.tile_bits = kMemoryTileBits;
+  a.tile_bits = kFewTileBits;
+  a.paged_bits = 2;
+  a.unit_tiles = 8;
   a.min_tiles = 2 * kWaves;
   a.run_bits = kRunBits;
   a.units = fast_div(even_units(a));

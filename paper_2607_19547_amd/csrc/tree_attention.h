@@ -66,18 +66,20 @@ struct MemoryArgs : SplitArgs {
   PackedView packed;
   const int32_t* blocks;  // packed pages of every request, or null
   int sinks, window;      // window 0: every key is seen
+  int paged_bits;         // a key tile of ordinary pages counts as 2^paged_bits packed ones in the cutting of the work
+  int unit_tiles;         // and a unit's start and end as that many
 };
 // Keys of a request that lie in packed pages: whole pages of cached tokens.
 __device__ __forceinline__ int packed_keys(const MemoryArgs& a, const Request& q, int b) {
   if (!a.blocks) return 0;
-  const scalar_ptr n = (scalar_ptr)(uint64_t)a.blocks;
-  return min(min(max(n[b], 0), a.t.page.div(q.cached)), a.t.max_blocks) * a.t.page.d;
+  return min(min(max(a.blocks[b], 0), a.t.page.div(q.cached)), a.t.max_blocks) * a.t.page.d;
 }
 // Whether a key of the table lies in a page of its pool.
 __device__ __forceinline__ bool in_pool(const MemoryArgs& a, int b, int key, int packed) {
   const int32_t pg = a.t.table[(int64_t)b * a.t.max_blocks + a.t.page.div(key)];
   return (unsigned)pg < (unsigned)(key < packed ? a.packed.n_pages : a.t.pool.n_pages);
 }
+constexpr int kFewTileBits = 5, kWideTileBits = 6;  // key tiles of 32 (a block of values) and of 64 keys
 // What a row tile (rows [i0, i1]) leaves out between the sinks and its rows'
 // windows, in whole key tiles of 2^BITS: tile t of its work is key tile t, or t + skip
 // from `sinks` on.  Keys below `low`, and from `high` on, are hidden from no row of it
@@ -85,6 +87,8 @@ __device__ __forceinline__ bool in_pool(const MemoryArgs& a, int b, int key, int
 struct Span {
   int sinks, skip, low, high;
   __device__ __forceinline__ int tile(int t) const { return t >= sinks ? t + skip : t; }
+  // of the tiles that the work has, those before key tile `key_tile`
+  __device__ __forceinline__ int before(int key_tile) const { return key_tile <= sinks ? key_tile : max(key_tile - skip, sinks); }
 };
 template <int BITS>
 __device__ __forceinline__ Span span_of(const MemoryArgs& a, const Request& q, int i0, int i1) {
@@ -169,19 +173,26 @@ __device__ __forceinline__ int key_tiles(const SplitArgs& a, uint32_t keys) {
   return max((int)((keys + (1 << a.tile_bits) - 1) >> a.tile_bits), 1);
 }
 template <bool PAIRS, class A>
-__device__ __forceinline__ Units unit_sizes(const A& a, const Request& q) {
+__device__ __forceinline__ Units unit_sizes(const A& a, const Request& q, int b) {
   Units s;
   s.units = s.nrt = (int)(((int64_t)q.n * a.t.G + (1 << a.row_bits) - 1) >> a.row_bits);
   s.ntile = key_tiles(a, q.len);
-  bool whole = true;  // row tiles see everything before them
+  bool whole = true;  // row tiles see everything before them (and are to be paired)
   if constexpr (A::kMemory) {
+    int packed = packed_keys(a, q, b) >> a.tile_bits;
     if (a.window) {
       // the sinks, and as many keys as the windows of a row tile's rows (n - 1 more at most) cover
       const int rows = a.t.mask ? q.n : min(q.n, (int)a.group.div((1 << a.row_bits) - 1) + 2);
       const int64_t keys = (int64_t)a.window + rows, tiles = (int64_t)min(a.sinks, q.len) + (1 << a.tile_bits) - 1 >> a.tile_bits;
       s.ntile = (int)min((int64_t)s.ntile, tiles + (keys + (2 << a.tile_bits) >> a.tile_bits));
       whole = false;
+      // (later row tiles leave out more: the last has the fewest packed tiles)
+      const int i0 = s.nrt ? a.group.div((s.nrt - 1) << a.row_bits) : 0;
+      packed = a.tile_bits == kWideTileBits ? span_of<kWideTileBits>(a, q, i0, i0).before(packed) : span_of<kFewTileBits>(a, q, i0, i0).before(packed);
     }
+    packed = min(packed, s.ntile);
+    if (a.paged_bits) whole = false;  // (a pair's tiles count as one each)
+    s.ntile = (int)min(packed + ((int64_t)(s.ntile - packed) << a.paged_bits), (int64_t)1 << 29);
   }
   if (PAIRS && whole && !a.t.mask && s.nrt > 1) {
     // the keys of both: the last rows of p and nrt - 1 - p are, added up, at most n + 2 row tiles' rows
@@ -193,6 +204,7 @@ __device__ __forceinline__ Units unit_sizes(const A& a, const Request& q) {
       s.ntile = pair;
     }
   }
+  if constexpr (A::kMemory) s.ntile += a.unit_tiles;
   return s;
 }
 __device__ __forceinline__ int64_t request_tiles(const SplitArgs& a, const Units& s) {
@@ -217,6 +229,13 @@ __device__ __forceinline__ Place place_at(const A& a, const Request& q, const Un
   x.h = s.units == 1 ? u : uniform(u / s.units);
   x.rt = u - x.h * s.units;
   x.n = s.ntile;
+  if constexpr (A::kMemory) {
+    x.n -= a.unit_tiles;
+    if (x.t0 >= x.n && !(PAIRS && s.units != s.nrt)) {
+      x.n = 0;
+      x.t0 = s.ntile - x.t0;
+    }
+  }
   if (PAIRS && s.units != s.nrt) {
     const int vectors = q.n * a.t.G;
     auto tiles = [&](int rt) {
@@ -267,7 +286,7 @@ __device__ __forceinline__ int run_of(int x, int64_t total, int64_t len) {
 template <bool PAIRS, bool BLOCK = false, class A>
 __device__ __forceinline__ bool find_run(const A& a, int w, Run* run) {
   if (a.t.B == 1) {
-    run->total = request_tiles(a, unit_sizes<PAIRS>(a, load_request_scalar(a.t, 0)));
+    run->total = request_tiles(a, unit_sizes<PAIRS>(a, load_request_scalar(a.t, 0), 0));
     const int64_t len = run_length(a, run->total);
     if (BLOCK && a.by_xcd) w = run_of(w, run->total, len);
     run->w = w;
@@ -277,7 +296,7 @@ __device__ __forceinline__ bool find_run(const A& a, int w, Run* run) {
     return run->begin < run->total;
   }
   const int lane = threadIdx.x & 63, per = (a.t.B + 63) >> 6;
-  auto tiles = [&](int b) { return request_tiles(a, unit_sizes<PAIRS>(a, load_request(a.t, b))); };
+  auto tiles = [&](int b) { return request_tiles(a, unit_sizes<PAIRS>(a, load_request(a.t, b), b)); };
   const int b0 = min(lane * per, a.t.B), b1 = min(b0 + per, a.t.B);
   int64_t sum = 0;
 #pragma unroll 4
@@ -295,7 +314,7 @@ __device__ __forceinline__ bool find_run(const A& a, int w, Run* run) {
   int b = at * per;
   if (per > 1)  // (the whole wavefront walks, off the scalar cache)
     for (; b < a.t.B - 1; ++b) {
-      const int64_t x = request_tiles(a, unit_sizes<PAIRS>(a, load_request_scalar(a.t, b)));
+      const int64_t x = request_tiles(a, unit_sizes<PAIRS>(a, load_request_scalar(a.t, b), b));
       if (off < x) break;
       off -= x;
     }
@@ -354,8 +373,10 @@ inline int even_units(const SplitArgs& a) {
 }
 // Workgroups that a launch needs at most: the runs there can be, from the rows
 // and the block tables' room.  A batch with room for one run needs no merge.
-inline int most_runs(const SplitArgs& a) {
-  const double tiles = std::max<double>(1, ((double)a.t.max_blocks * a.t.page.d + (1 << a.tile_bits) - 1) / (1 << a.tile_bits));
+template <class A>
+inline int most_runs(const A& a) {
+  double tiles = std::max<double>(1, ((double)a.t.max_blocks * a.t.page.d + (1 << a.tile_bits) - 1) / (1 << a.tile_bits));
+  if constexpr (A::kMemory) tiles = tiles * (1 << a.paged_bits) + a.unit_tiles;
   const double units = ((double)a.t.n_rows * a.t.G / (1 << a.row_bits) + a.t.B) * a.t.Hkv;
   return (int)std::min<double>(1 << a.run_bits, std::max<double>(a.units.d, ceil(tiles * units / a.min_tiles)));
 }
@@ -390,7 +411,7 @@ inline TreeArgs tree_args(const Geo& g, const cs_page_pool& pool, int layer, con
 }
 
 // The instance for many rows (bf16, head_dim 128): see tree_attention_wide.hip.
-constexpr int kWideRowBits = 8, kWideTileBits = 6, kWideRunBits = 8;
+constexpr int kWideRowBits = 8, kWideRunBits = 8;
 size_t tree_wide_workspace();
 // once: keys and values with the non-temporal hint.  One row tile a request: 32 requests
 // of 8,000 tokens, 8 rows 72 -> 64 us; two and more read them again (tree-sized steps

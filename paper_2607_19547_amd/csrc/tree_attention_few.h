@@ -46,8 +46,7 @@ __device__ __forceinline__ void put_elem(uint16_t* p, float x) { *p = f32_to_bf1
 // load and a prefix sum).
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
-// Packed pages: a key tile of the work has 32 keys, a block of values.
-constexpr int kMemoryTileBits = 5, kMemoryTile = 1 << kMemoryTileBits;
+constexpr int kMemoryTile = 1 << kFewTileBits;  // (packed pages)
 // The running maximum may grow by 2^5 before the accumulators are rescaled:
 // probabilities stay far inside the range of both types.
 constexpr float kRescaleLog2 = 5.f;
@@ -103,7 +102,7 @@ __device__ __forceinline__ Place next_place(const A& a, int* b, int64_t* off, in
 #pragma unroll 1
   while (*b < a.t.B && *left > 0) {
     *q = load_request_scalar(a.t, *b);
-    const Units units = unit_sizes<PAIRS>(a, *q);
+    const Units units = unit_sizes<PAIRS>(a, *q, *b);
     if (*off >= request_tiles(a, units)) {
       *off = 0;
       ++*b;
@@ -175,13 +174,18 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const Args) {
     const int i_last = a.group.div(min(rt * RT + RT, vectors) - 1);
     const int key_end = t.mask ? q.len : min(q.len, q.cached + i_last + 1);
     Span span;
-    int t_begin = t0, t_end = min(t0 + seg, (key_end + KT - 1) / KT), packed_end = 0;  // (tiles of KT keys; packed ones, of 32)
+    int t_begin = t0, t_end = min(t0 + seg, (key_end + KT - 1) / KT), first_tile = t0, packed_end = 0;  // (tiles of KT keys; packed ones, of 32)
     if constexpr (kMemory) {
-      span = span_of<kMemoryTileBits>(a, q, a.group.div(rt * RT), i_last);
-      const int end = min(t0 + seg, (key_end + kMemoryTile - 1) / kMemoryTile - span.skip);
-      const int packed = packed_keys(a, q, b) >> kMemoryTileBits;
-      packed_end = min(end, packed <= span.sinks ? packed : max(packed - span.skip, span.sinks));
-      t_begin = max(t0, packed_end) * kSub;
+      span = span_of<kFewTileBits>(a, q, a.group.div(rt * RT), i_last);
+      const int last = (key_end + kMemoryTile - 1) / kMemoryTile - span.skip;
+      const int packed = span.before(packed_keys(a, q, b) >> kFewTileBits);
+      auto tile_at = [&](int t) {  // of a place in the cut work
+        return min(t <= packed ? t : packed + ((t - packed + (1 << a.paged_bits) - 1) >> a.paged_bits), last);
+      };
+      const int begin = tile_at(t0), end = tile_at(t0 + seg);
+      first_tile = begin;
+      packed_end = min(end, packed);
+      t_begin = max(begin, packed_end) * kSub;
       t_end = end * kSub;
     }
     auto key_of = [&](int tile) {  // the first key of a tile
@@ -343,7 +347,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const Args) {
       auto fetch_page4 = [&](int tile) { page4 = pages[page_div.div(span.tile(min(tile, packed_end - 1)) * kMemoryTile)]; };
       __amdgpu_buffer_rsrc_t codes, scales;
       auto place4 = [&](int tile) -> bool {
-        const int key = span.tile(tile) * kMemoryTile, x = (key - page_div.div(key) * page_div.d) >> kMemoryTileBits;
+        const int key = span.tile(tile) * kMemoryTile, x = (key - page_div.div(key) * page_div.d) >> kFewTileBits;
         const bool have = tile < packed_end && (unsigned)page4 < (unsigned)pk.n_pages;
         const char* p = pk.base + page4 * pk.page_bytes + plane4;  // (no bytes: no address is used)
         const int c = x * (kMemoryTile * D / 2), s = x * D;
@@ -429,7 +433,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const Args) {
         }
       };
       Tile T;
-      int tile = t0 + wave;
+      int tile = first_tile + wave;
       if (tile < packed_end) {
         fetch_page4(tile);
         T.have = place4(tile);
@@ -793,7 +797,7 @@ __global__ __launch_bounds__(kThreads) void tree_combine(const Args a) {
   Run run;
   if (!find_run<PAIRS>(a, w1, &run)) return;
   const Request q = load_request_scalar(t, run.b);
-  const Place at = place_at<PAIRS>(a, q, unit_sizes<PAIRS>(a, q), run.off);
+  const Place at = place_at<PAIRS>(a, q, unit_sizes<PAIRS>(a, q, run.b), run.off);
   if (at.t0 == 0 || at.n == 0) return;  // the border lies between row tiles
   const int h = at.h, rt = at.rt;
   const int64_t len = run_length(a, run.total), unit0 = run.begin - at.t0, unit1 = unit0 + at.n;

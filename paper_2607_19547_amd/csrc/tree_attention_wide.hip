@@ -131,7 +131,7 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const Args a0) 
       const Args A = args();
       if (b >= A.t.B) break;  // (lengths that changed meanwhile)
       q = load_request_scalar(A.t, b);
-      const Units units = unit_sizes<true>(A, q);
+      const Units units = unit_sizes<true>(A, q, b);
       if (off >= request_tiles(A, units)) {  // behind this request's units
         off = 0;
         ++b;
@@ -548,7 +548,7 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const Args a0) 
     if constexpr (kMemory) {
       auto place = [&](int keys) {  // of the first tile that begins at `keys` or behind it, among the unit's
         const int x = (keys + kKT - 1) / kKT;
-        return x <= span.sinks ? x : max(x - span.skip, span.sinks);
+        return span.before(x);
       };
       if (!bad) {
         if (span.high > span.low) clear0 = min((max(place(span.high) - t0, 0) + 3) & ~3, n_kt);
@@ -689,7 +689,7 @@ __global__ __launch_bounds__(kStripThreads) void tree_combine_wide(const Args a)
   Run run;
   if (!find_run<true>(a, w1, &run)) return;
   const Request q = load_request_scalar(t, run.b);
-  const Place at = place_at<true>(a, q, unit_sizes<true>(a, q), run.off);
+  const Place at = place_at<true>(a, q, unit_sizes<true>(a, q, run.b), run.off);
   if (at.t0 == 0 || at.n == 0) return;  // the border lies between row tiles
   const int h = at.h, rt = at.rt;
   const int64_t len = run_length(a, run.total), unit0 = run.begin - at.t0;
