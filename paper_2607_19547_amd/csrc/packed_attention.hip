@@ -133,12 +133,45 @@ static bool has_instance(const Geo& g) {
   if (g.dtype == CS_BF16) return g.D == 32 || g.D == 64 || g.D == 96 || g.D == 128 || g.D == 256;
   return g.D == 16 || g.D == 32 || g.D == 64 || g.D == 128;
 }
-static int most_row_groups(const Geo& g) { return g.D > 128 || g.D * g.esize > 256 ? 1 : g.D * g.esize > 128 ? 2 : 4; }
 
-// Whether the kernel for many rows (bf16 x 128) takes the batch.
-static bool wide(const Geo& g, const cs_batch& b) {
-  const int64_t qv = (int64_t)(b.max_rows > 0 ? b.max_rows : b.n_rows) * g.G;
-  return g.dtype == CS_BF16 && g.D == 128 && qv > 64;
+// Which kernel and row tile takes a batch, by the key tiles (of 32, over all requests
+// and KV heads) that the block tables have room for and the windows let be seen, and the
+// row tiles of 16 query vectors that each of them meets.  The host does not know the
+// lengths, and tables are seldom filled: borders are put at 1.6 times what was
+// measured on filled ones.
+struct Work {
+  double tiles, row_tiles, row_tiles_wide;  // (of 256)
+};
+static Work work_of(const Geo& g, const cs_batch& b, int sinks, int window) {
+  const double rows = b.max_rows > 0 ? b.max_rows : b.n_rows, vectors = rows * g.G;
+  double keys = (double)b.max_blocks * g.T;
+  if (window) keys = std::min(keys, (double)sinks + window + std::min(rows, 32.));  // (a row tile's rows, about)
+  return {b.n_requests * keys * g.Hkv / 32, ceil(vectors / 16), ceil(vectors / 256)};
+}
+// Row tiles of 32 or 64 convert a packed tile half or a quarter as often, in fewer and
+// longer pieces of work.  Measured, tiles x row tiles of 16 and us with row tiles of 16 /
+// 32 / 64: bf16 x 64 33,000 23.7 / 27.1 / 32.8, 67,000 39.8 / 37.6 / 43.3, 131,000 59.7 /
+// 51.4 / 52.4, 809,000 337 / 219 / 191; x 32 33,000 21.3 / 25.3 / 27.3, 131,000 50.0 / 46.0 / 43.7;
+// x 96 9,000 21.8 / 22.4, 19,000 33.0 / 30.3, 131,000 121 / 77; float32 x 64 67,000 51.6 / 51.5,
+// 131,000 78.7 / 76.2; x 32 66,000 43.9 / 41.2 / 47.9, 131,000 66.3 / 60.6 / 63.8.  Row tiles of 32
+// spill registers with bf16 x 128 (which has the kernel for many rows), x 256 and float32 x 128.
+static int most_row_groups(const Geo& g) {
+  if (g.dtype == CS_F32) return g.D <= 64 ? 2 : 1;
+  return g.D <= 64 ? 4 : g.D <= 96 ? 2 : 1;
+}
+static int row_groups(const Geo& g, const Work& w) {
+  const double n = w.tiles * w.row_tiles;
+  if (w.row_tiles <= 1 || n < 1.6 * (g.D == 96 ? 12e3 : 55e3)) return 1;
+  return std::min(most_row_groups(g), n < 1.6 * 200e3 ? 2 : 4);
+}
+// The kernel for many rows (bf16 x 128) takes 5 ns for a key tile and 256 query vectors
+// on the whole GPU, row tiles of 16 take 0.56 ns each, and it starts and ends 10 us
+// later.  Measured (us, row tiles of 16 / it): 65,536 tokens, 17 rows 38.6 / 45.4, 64 rows
+// 84 / 62; 16,384 tokens, 64 rows 31.7 / 36.6; 8 requests of 4,096, 64 rows 53 / 46; 32 of
+// 8,192, 4 rows 35 / 69; 8,192 tokens, 250 rows 56 / 46; 1,024 tokens, 250 rows 23.1 / 25.6; 1,999 rows
+// that see 1,024 tokens each 109 / 54 (8 query heads for each of 2).
+static bool wide(const Geo& g, const Work& w) {
+  return g.dtype == CS_BF16 && g.D == 128 && w.tiles * (0.56 * w.row_tiles - 5 * w.row_tiles_wide) > 1.6 * 10e3;
 }
 
 size_t packed_attend_workspace(const Geo& g) {
@@ -147,12 +180,12 @@ size_t packed_attend_workspace(const Geo& g) {
   return std::max(few, tree_attend_workspace(g));  // (a call without packed pages and window is that one)
 }
 
-template <typename E, int D, int NR, bool ONCE>
+template <typename E, int D, int NR>
 static void run_split(const MemoryArgs& a, hipStream_t s) {
   const int runs = most_runs(a);
   {
     TraceScope tr("packed_attend", s);
-    CS_LAUNCH(tr, (tree_attend<E, D, NR, ONCE, MemoryArgs>), dim3(NR > 1 ? (runs + 7) / 8 * 8 : runs), dim3(kThreads), 0, s, a);
+    CS_LAUNCH(tr, (tree_attend<E, D, NR, false, MemoryArgs>), dim3(NR > 1 ? (runs + 7) / 8 * 8 : runs), dim3(kThreads), 0, s, a);
   }
   if (runs == 1) return;
   TraceScope tr("packed_combine", s);
@@ -160,11 +193,12 @@ static void run_split(const MemoryArgs& a, hipStream_t s) {
 }
 template <typename E, int D>
 static void run_split(const MemoryArgs& a, int nr, hipStream_t s) {
-  if constexpr (D * sizeof(E) <= 128)
-    if (nr == 4) return run_split<E, D, 4, false>(a, s);
-  if constexpr (D * sizeof(E) <= 256 && D <= 128)
-    if (nr == 2) return run_split<E, D, 2, false>(a, s);
-  run_split<E, D, 1, false>(a, s);
+  constexpr bool kBf16 = sizeof(E) == 2;
+  if constexpr (kBf16 && D <= 64)
+    if (nr == 4) return run_split<E, D, 4>(a, s);
+  if constexpr (D <= (kBf16 ? 96 : 64))
+    if (nr == 2) return run_split<E, D, 2>(a, s);
+  run_split<E, D, 1>(a, s);
 }
 
 cs_status launch_packed_attend(const Geo& g, const cs_page_pool& pool, const cs_packed_pool* packed, int layer,
@@ -191,13 +225,14 @@ cs_status launch_packed_attend(const Geo& g, const cs_page_pool& pool, const cs_
     return check_launch("packed attention launch");
   }
   if (check_only) return CS_OK;
-  a.paged_bits = a.unit_tiles = 0;
-  if (wide(g, b) && low_o % 16 == 0) {
+  a.paged_bits = 0;
+  a.unit_tiles = 5;
+  const Work w = work_of(g, b, job.sinks, job.window);
+  if (wide(g, w) && low_o % 16 == 0) {
     launch_packed_wide(a, ws, false, s);
     return check_launch("packed attention launch");
   }
-  const int64_t qv = (int64_t)(b.max_rows > 0 ? b.max_rows : b.n_rows) * g.G;
-  const int nr = std::min(most_row_groups(g), qv <= 16 ? 1 : qv <= 256 ? 2 : 4);
+  const int nr = row_groups(g, w);
   a.row_bits = nr == 1 ? 4 : nr == 2 ? 5 : 6;
   a.tile_bits = kFewTileBits;
   a.paged_bits = 2;

@@ -204,11 +204,6 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const Args) {
 #pragma unroll
       for (int k = 0; k < KS; ++k) qf[x][k] = *(const Words<16>*)piece(qp, k);
     }
-    Hidden hidden[NR];  // the keys that the row's window leaves out
-    if constexpr (kMemory) {
-#pragma unroll
-      for (int x = 0; x < NR; ++x) hidden[x] = hidden_keys(a, q, row[x]);
-    }
 
     // Where the 16-key pieces of a tile lie: 16 rows of a page (pages are
     // multiples of 16 tokens), as many of them as the request has; none behind
@@ -473,9 +468,10 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const Args) {
         const bool masked = !have || (key0 + kMemoryTile > span.low && key0 < span.high);
         uint32_t vis[NR];  // bit j: key 8 lg + j
         if (masked) {
+          const Args A = args();
 #pragma unroll
           for (int x = 0; x < NR; ++x) {
-            vis[x] = have ? ~(uint32_t)hidden[x].bits(key0, kMemoryTile) : 0u;
+            vis[x] = have ? ~(uint32_t)hidden_keys(A, q, row[x]).bits(key0, kMemoryTile) : 0u;
             seen[x] = seen[x] || vis[x];
             vis[x] >>= 8 * lg;
 #pragma unroll
@@ -616,7 +612,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const Args) {
           }
           if (w0 < 0) bits = -w0 >= 64 ? ~0ull : bits << -w0 | ((1ull << -w0) - 1);
           vis[x] = (uint32_t)bits & there;
-          if constexpr (kMemory) vis[x] &= ~(uint32_t)hidden[x].bits(key0, KT);
+          if constexpr (kMemory) vis[x] &= ~(uint32_t)hidden_keys(A, q, row[x]).bits(key0, KT);
           seen[x] = seen[x] || vis[x];
           vis[x] >>= 4 * lg;
 #pragma unroll

@@ -69,6 +69,7 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const Args a0) 
   __shared__ __attribute__((aligned(1024))) char lo_v0[kKT * kRow], lo_v1[kKT * kRow], lo_v2[kKT * kRow], lo_v3[kKT * kRow];
   __shared__ __attribute__((aligned(1024))) char up_k0[kKT * kRow], up_k1[kKT * kRow], up_k2[kKT * kRow], up_k3[kKT * kRow];
   __shared__ __attribute__((aligned(1024))) char up_staged[kMemory ? 3 * kWideWaves * kStagedBytes : 4];
+  __shared__ int up_odd[kMemory ? kWideWaves : 1];
   auto kbuf = [&](auto B) -> char* {
     if constexpr (decltype(B)::value == 0) return up_k0;
     else if constexpr (decltype(B)::value == 1) return up_k1;
@@ -209,17 +210,22 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const Args a0) 
     // all eight.
     const char* p_plane = nullptr;
     int64_t packed_bytes = 0;
-    int n_packed = 0, page_codes = 0;
+    int n_packed = 0, page_codes = 0, packed_end = 0;  // (tiles of the piece whose keys of this wavefront are packed)
     if constexpr (kMemory) {
+      // keys [64 t + 8 wave, + 8) of key tile t
+      packed_end = min(max(span.before((packed - 8 * wave + kKT - 1) / kKT) - t0, 0), n_kt);
       const Args A = args();
       p_plane = A.packed.base + ((int64_t)A.t.layer * A.t.Hkv + h) * A.packed.plane_bytes();
       packed_bytes = A.packed.page_bytes;
       n_packed = A.packed.n_pages;
     }
-    auto is_packed = [&](int i) { return kMemory && i < n_kt && key_of(i) < packed; };
-    auto staged = [&](int i) -> char* { return up_staged + (i % 3 * kWideWaves + wave) * kStagedBytes; };
+    auto is_packed = [&](int i) { return kMemory && i < packed_end; };
+    char* const staged = up_staged + wave * kStagedBytes;  // place i of 3 at + i * kStagedTile
+    constexpr int kStagedTile = kWideWaves * kStagedBytes;
+    int put_at = 0, load_at = 0;  // of the next tile that is put, and loaded
+    auto turn = [](int& at) { at = at == 2 * kStagedTile ? 0 : at + kStagedTile; };
     auto find_codes = [&](int i) {
-      if (packed > 0) page_codes = table[page.div(min(key_of(i), packed - 1))];
+      if (i < packed_end) page_codes = table[page.div(key_of(i))];
     };
     auto load_codes = [&](int i) {
       const PackedView pv = {nullptr, 0, 0, page.d, 128};
@@ -232,15 +238,17 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const Args a0) 
       // 512 bytes of key codes, 512 of value codes; 4 x 8 bytes of key scales, 128 of value scales
       const int at = x < 32 ? 16 * x : pv.v_codes() - 512 + 16 * x;
       const int as = x < 8 ? pv.k_scales() + (in_page & 31) + 16 * x - 12 * (x & 1) : pv.v_scales() - 32 + 4 * x;
-      char* to = staged(i);
+      char* to = staged + load_at;
+      turn(load_at);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rc, (lds_void*)to, 16, at, 0, 0, ONCE ? kNonTemporal : 0);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(to + 1024), 4, as, 0, 0, ONCE ? kNonTemporal : 0);
       find_codes(i + 1);
     };
-    auto put_codes = [&](int i, char* Kd, char* Vd) {
+    auto put_codes = [&](char* Kd, char* Vd) {
       int x = lane;
       asm volatile("" : "+v"(x));
-      const char* from = staged(i);
+      const char* from = staged + put_at;
+      turn(put_at);
       const int r = 8 * wave + (x >> 3), c = 2 * (x & 7);
       const u32x2 kc = *(const u32x2*)(from + 8 * x), vc = *(const u32x2*)(from + 512 + 8 * x);
       const float ks = scale_of<0>(*(const uint8_t*)(from + 1024 + 4 * (x & 6) + (x >> 3)));
@@ -268,21 +276,17 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const Args a0) 
     };
     // Step i's part of the ring's filling: tile i + 3 of ordinary pages is fetched;
     // packed, tile i + 2 is put there and tile i + 4 loaded.
-    auto fill = [&](int i, char* K2, char* V2, char* K3, char* V3) {
-      if constexpr (kMemory) {
-        if (is_packed(i + 2)) {
-          // (behind its loads are those of tile i + 3, if any)
-          if (is_packed(i + 3)) asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
-          else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-          put_codes(i + 2, K2, V2);
-          if (is_packed(i + 4)) load_codes(i + 4);
-        }
-        if (is_packed(i + 3)) {
-          find_page(i + 4);
-          return;
-        }
-      }
-      fetch(i + 3, K3, V3);
+    auto fill_packed = [&](int i, char* K2, char* V2) {
+      if (!is_packed(i + 2)) return;
+      // (behind its loads are those of tile i + 3)
+      if (is_packed(i + 3)) asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
+      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      put_codes(K2, V2);
+      if (is_packed(i + 4)) load_codes(i + 4);
+    };
+    auto fill = [&](int i, char* K3, char* V3) {
+      if (!is_packed(i + 3)) fetch(i + 3, K3, V3);
+      else if (!is_packed(i + 4)) find_page(i + 4);
     };
     if constexpr (kMemory) {
       find_codes(0);
@@ -290,13 +294,28 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const Args a0) 
       for (int i = 0; i < 3; ++i)
         if (is_packed(i)) load_codes(i);
     }
-    auto fetch_first = [&](int i, char* Kd, char* Vd) {
-      if (is_packed(i)) find_page(i + 1);
-      else fetch(i, Kd, Vd);
+    // With windows the tiles that every row sees whole begin at tile clear0; that
+    // one is to be in the ring's first slot, where the loop over them begins.
+    int clear0 = 0, ring0 = 0;
+    if constexpr (kMemory) {
+      if (span.high > span.low) clear0 = min(max(span.before((span.high + kKT - 1) / kKT) - t0, 0), n_kt);
+      ring0 = -clear0 & 3;
+    }
+    auto k_at = [&](int i) -> char* {
+      const int x = i + ring0;
+      return x & 2 ? (x & 1 ? up_k3 : up_k2) : (x & 1 ? up_k1 : up_k0);
+    };
+    auto v_at = [&](int i) -> char* {
+      const int x = i + ring0;
+      return x & 2 ? (x & 1 ? lo_v3 : lo_v2) : (x & 1 ? lo_v1 : lo_v0);
+    };
+    auto fetch_first = [&](int i) {
+      if (!is_packed(i)) fetch(i, k_at(i), v_at(i));
+      else if (!is_packed(i + 1)) find_page(i + 1);
     };
     find_page(0);
-    fetch_first(0, up_k0, lo_v0);
-    fetch_first(1, up_k1, lo_v1);
+    fetch_first(0);
+    fetch_first(1);
     {
       const Args A = args();
       const int qv = min(rt * 256 + 32 * wave + ql, q.n * A.t.G - 1);
@@ -317,12 +336,12 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const Args a0) 
         for (int x = p0 + tid; x <= p1; x += kWideThreads) bad |= tb[x] < 0 || tb[x] >= A.t.pool.n_pages;
       }
     }
-    fetch_first(2, up_k2, lo_v2);
+    fetch_first(2);
     if constexpr (kMemory) {
       if (is_packed(0)) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        put_codes(0, up_k0, lo_v0);
-        if (is_packed(1)) put_codes(1, up_k1, lo_v1);
+        put_codes(k_at(0), v_at(0));
+        if (is_packed(1)) put_codes(k_at(1), v_at(1));
         if (is_packed(3)) load_codes(3);
       }
     }
@@ -407,14 +426,27 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const Args a0) 
     // are rescaled for the tile: their first factor is 0.)
     auto not_finite = [&](char* V, int kt) {
       uint32_t odd = 0;
-      int x = lane;
+      int x = kMemory ? tid : lane;
       asm volatile("" : "+v"(x));  // (worked out here, not kept through the tiles)
-      for (; x < kKT * kRow / 16; x += 64) {
+      for (; x < kKT * kRow / 16; x += kMemory ? kWideThreads : 64) {
         const u32x4 v = *(const u32x4*)(V + 16 * x);
 #pragma unroll
         for (int y = 0; y < 4; ++y) odd |= (v[y] & 0x7f807f80u) + 0x00800080u;
       }
-      if (__ballot(odd & 0x80008000u)) {
+      bool found = __ballot(odd & 0x80008000u) != 0;
+      if constexpr (kMemory) {
+        // Windows have more such tiles: the wavefronts share one.  (A barrier that
+        // waits for no loads; the step's end has the one before the next tile's flags.)
+        if (lane == 0) up_odd[wave] = found;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        int any = 0;
+#pragma unroll
+        for (int w = 0; w < kWideWaves; ++w) any |= up_odd[w];
+        found = uniform(any);
+      }
+      if (found) {
         const uint64_t mine = visible(kt);
 #pragma unroll 1
         for (int sign = 0; sign < 2; ++sign) {
@@ -531,36 +563,27 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const Args a0) 
     };
     auto next = [](auto B) { return std::integral_constant<int, (decltype(B)::value + 1) & 3>{}; };
     auto step = [&](auto C, auto N, auto S, int i, f32x16& c0, f32x16& c1, f32x16& n0, f32x16& n1) {
-      fill(i, kbuf(next(N)), vbuf(next(N)), kbuf(S), vbuf(S));
+      fill(i, kbuf(S), vbuf(S));
       if (w_seen >= 0) {
         qk_head(kbuf(N), n0, n1);
         tile_max(c0, c1);
         exp_pv_qk(vbuf(C), kbuf(N), c0, c1, n0, n1);
       }
+      if constexpr (kMemory) fill_packed(i, kbuf(next(N)), vbuf(next(N)));
       landed();
     };
     // First the tiles that every row sees whole, their ring slots known to the
     // compiler, a tile's scores computed a step ahead; then, in a plain loop, the
     // few with the step's own rows.
-    // With windows there are masked ones before them, too, as many as the ring has
-    // slots or a multiple of that.
-    int n_clear = 0, clear0 = 0;  // tiles [clear0, n_clear)
+    // With windows there are masked ones before them, too.
+    int n_clear = 0;  // the end of them
     if constexpr (kMemory) {
-      auto place = [&](int keys) {  // of the first tile that begins at `keys` or behind it, among the unit's
-        const int x = (keys + kKT - 1) / kKT;
-        return span.before(x);
-      };
-      if (!bad) {
-        if (span.high > span.low) clear0 = min((max(place(span.high) - t0, 0) + 3) & ~3, n_kt);
-        n_clear = min(max(place(all_see / kKT * kKT) - t0, clear0), n_kt);
-      }
+      n_clear = bad ? clear0 : min(max(span.before(all_see / kKT) - t0, clear0), n_kt);
     } else {
       n_clear = bad ? 0 : min(max(all_see / kKT - t0, 0), n_kt);
     }
     f32x16 sa0, sa1, sb0, sb1;
     landed();  // tiles 0 and 1 and the queries
-    auto k_at = [&](int x) -> char* { return x & 2 ? (x & 1 ? up_k3 : up_k2) : (x & 1 ? up_k1 : up_k0); };
-    auto v_at = [&](int x) -> char* { return x & 2 ? (x & 1 ? lo_v3 : lo_v2) : (x & 1 ? lo_v1 : lo_v0); };
 #pragma unroll 1
     for (int pass = kMemory ? 0 : 1; pass < 2; ++pass) {
       if (pass) {
@@ -580,7 +603,8 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const Args a0) 
 #pragma unroll 1
       for (int i = pass ? n_clear : 0; i < (pass ? n_kt : clear0); ++i) {
         const int kt = kMemory ? span.tile(t0 + i) * kKT : key_begin + i * kKT;
-        fill(i, k_at(i + 2), v_at(i + 2), k_at(i + 3), v_at(i + 3));
+        if constexpr (kMemory) fill_packed(i, k_at(i + 2), v_at(i + 2));
+        fill(i, k_at(i + 3), v_at(i + 3));
         char* V = v_at(i);
         if (kt <= w_seen) {
           qk(k_at(i), sa0, sa1);

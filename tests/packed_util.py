@@ -74,9 +74,27 @@ def tol(out, lse, spread, dtype):
         return t, rel + 2.0 ** -23 * np.abs(np.where(np.isfinite(lse), lse, 0))
 
 
+def row_hints(case):
+    """Values of max_rows that make the call take its other kernels: with the most rows the largest row tiles (or, in
+    bf16 with heads of 128, the kernel for many rows), with some the row tiles of 32."""
+    keys = case.max_blocks * case.page
+    if case.window:
+        keys = min(keys, case.sinks + case.window + 32)
+    tiles = max(1.0, len(case.cached) * keys * case.hkv / 32)
+    some = int(200e3 / tiles * 16 / (case.hq // case.hkv)) + 1
+    return (0, 2_000_000) if case.d > 64 else (0, some, 2_000_000)
+
+
 def check(case, b, layer=1, what="", **kw):
+    ref = case.attend_ref(layer)
+    for hint in row_hints(case):
+        out, lse = _check(case, b, layer, f"{what} max_rows {hint}", ref, max_rows=hint, **kw)
+    return out, lse
+
+
+def _check(case, b, layer, what, ref, **kw):
     out, lse = (f64(x) for x in case.run(b, layer, **kw))
-    ref, ref_lse, spread = case.attend_ref(layer)
+    ref, ref_lse, spread = ref
     t_out, t_lse = tol(ref, ref_lse, spread, case.dtype)
     what = f"{what} packed {case.packed} cached {case.cached} new {case.new} {case.hq}/{case.hkv} x {case.d} " \
            f"{case.dtype} sinks {case.sinks} window {case.window}"
