@@ -164,6 +164,11 @@ static int row_groups(const Geo& g, const Work& w) {
   if (w.row_tiles <= 1 || n < 1.6 * (g.D == 96 ? 12e3 : 55e3)) return 1;
   return std::min(most_row_groups(g), n < 1.6 * 200e3 ? 2 : 4);
 }
+// Two packed tiles a step, with row tiles of 16, in place of one.  Measured (us, tiles of
+// memories that the cache does not hold, one / two): 12,000 23.7 / 26.0, 25,000 35.2 / 33.8,
+// 33,000 48 / 41, 66,000 72 / 67 and 77 / 68; x 64 66,000 50 / 44, float32 x 64 50 / 47; x 32 36.2 / 36.3.
+constexpr double kDeepTiles = 1.6 * 25e3;
+constexpr bool has_deep(bool bf16, int d) { return d == 64 || (bf16 && (d == 96 || d == 128)); }
 // The kernel for many rows (bf16 x 128) takes 5 ns for a key tile and 256 query vectors
 // on the whole GPU, row tiles of 16 take 0.56 ns each, and it starts and ends 10 us
 // later.  Measured (us, row tiles of 16 / it): 65,536 tokens, 17 rows 38.6 / 45.4, 64 rows
@@ -180,24 +185,26 @@ size_t packed_attend_workspace(const Geo& g) {
   return std::max(few, tree_attend_workspace(g));  // (a call without packed pages and window is that one)
 }
 
-template <typename E, int D, int NR>
+template <typename E, int D, int NR, int PT = 1>
 static void run_split(const MemoryArgs& a, hipStream_t s) {
   const int runs = most_runs(a);
   {
     TraceScope tr("packed_attend", s);
-    CS_LAUNCH(tr, (tree_attend<E, D, NR, false, MemoryArgs>), dim3(NR > 1 ? (runs + 7) / 8 * 8 : runs), dim3(kThreads), 0, s, a);
+    CS_LAUNCH(tr, (tree_attend<E, D, NR, false, MemoryArgs, PT>), dim3(NR > 1 ? (runs + 7) / 8 * 8 : runs), dim3(kThreads), 0, s, a);
   }
   if (runs == 1) return;
   TraceScope tr("packed_combine", s);
   CS_LAUNCH(tr, (tree_combine<E, D, (NR > 1), MemoryArgs>), dim3(runs - 1, 2 * NR), dim3(kThreads), 0, s, a);
 }
 template <typename E, int D>
-static void run_split(const MemoryArgs& a, int nr, hipStream_t s) {
+static void run_split(const MemoryArgs& a, int nr, bool deep, hipStream_t s) {
   constexpr bool kBf16 = sizeof(E) == 2;
   if constexpr (kBf16 && D <= 64)
     if (nr == 4) return run_split<E, D, 4>(a, s);
   if constexpr (D <= (kBf16 ? 96 : 64))
     if (nr == 2) return run_split<E, D, 2>(a, s);
+  if constexpr (has_deep(kBf16, D))
+    if (deep) return run_split<E, D, 1, 2>(a, s);
   run_split<E, D, 1>(a, s);
 }
 
@@ -233,6 +240,7 @@ cs_status launch_packed_attend(const Geo& g, const cs_page_pool& pool, const cs_
     return check_launch("packed attention launch");
   }
   const int nr = row_groups(g, w);
+  const bool deep = w.tiles * w.row_tiles >= kDeepTiles;
   a.row_bits = nr == 1 ? 4 : nr == 2 ? 5 : 6;
   a.tile_bits = kFewTileBits;
   a.paged_bits = 2;
@@ -245,18 +253,18 @@ cs_status launch_packed_attend(const Geo& g, const cs_page_pool& pool, const cs_
   a.part_ml = a.part + 2 * ((size_t)kRuns << a.row_bits) * g.D;
   if (g.dtype == CS_BF16) {
     switch (g.D) {
-      case 32: run_split<uint16_t, 32>(a, nr, s); break;
-      case 64: run_split<uint16_t, 64>(a, nr, s); break;
-      case 96: run_split<uint16_t, 96>(a, nr, s); break;
-      case 128: run_split<uint16_t, 128>(a, nr, s); break;
-      default: run_split<uint16_t, 256>(a, nr, s);
+      case 32: run_split<uint16_t, 32>(a, nr, deep, s); break;
+      case 64: run_split<uint16_t, 64>(a, nr, deep, s); break;
+      case 96: run_split<uint16_t, 96>(a, nr, deep, s); break;
+      case 128: run_split<uint16_t, 128>(a, nr, deep, s); break;
+      default: run_split<uint16_t, 256>(a, nr, deep, s);
     }
   } else {
     switch (g.D) {
-      case 16: run_split<float, 16>(a, nr, s); break;
-      case 32: run_split<float, 32>(a, nr, s); break;
-      case 64: run_split<float, 64>(a, nr, s); break;
-      default: run_split<float, 128>(a, nr, s);
+      case 16: run_split<float, 16>(a, nr, deep, s); break;
+      case 32: run_split<float, 32>(a, nr, deep, s); break;
+      case 64: run_split<float, 64>(a, nr, deep, s); break;
+      default: run_split<float, 128>(a, nr, deep, s);
     }
   }
   return check_launch("packed attention launch");

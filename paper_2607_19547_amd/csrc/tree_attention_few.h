@@ -116,7 +116,10 @@ __device__ __forceinline__ Place next_place(const A& a, int* b, int64_t* off, in
   return x;
 }
 
-template <typename E, int D, int NR, bool ONCE, class Args = SplitArgs>
+// PT: packed tiles of a wavefront's step, all of them in flight while the step before
+// is worked on.  One does where there is little to do; much is bound by what is in
+// flight, which with a tile of 4 KB for each wavefront is too little for 5 TB/s.
+template <typename E, int D, int NR, bool ONCE, class Args = SplitArgs, int PT = 1>
 __global__ __launch_bounds__(kThreads, 2) void tree_attend(const Args) {
   constexpr bool kBf16 = sizeof(E) == 2;
   constexpr int SUB = kBf16 ? 2 : 1;             // 16-key pieces of a tile
@@ -314,6 +317,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const Args) {
         uint32_t k[2][KW], ks[KSW], v[NB][VW], vs[NB][(VW + 3) / 4];
         bool have;
       };
+      constexpr int NP = 8 * PT;  // scores of a lane per query vector
       bf16x8 qt[NR][KW][NT];
 #pragma unroll
       for (int x = 0; x < NR; ++x)
@@ -338,19 +342,25 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const Args) {
       const int k_off = 2 * ln * (D / 2) + (kRowRuns ? 4 * KW * lg : 4 * lg);
       const int v_off = pk.v_codes() + (lg * D + VW * ln) * 4, vs_off = pk.v_scales() + VW * ln;
       const int ks_off = pk.k_scales() + 2 * ln + (kRowRuns ? kBlock * (KW * lg / 4) : 0);
-      int page4 = 0;
-      auto fetch_page4 = [&](int tile) { page4 = pages[page_div.div(span.tile(min(tile, packed_end - 1)) * kMemoryTile)]; };
-      __amdgpu_buffer_rsrc_t codes, scales;
-      auto place4 = [&](int tile) -> bool {
-        const int key = span.tile(tile) * kMemoryTile, x = (key - page_div.div(key) * page_div.d) >> kFewTileBits;
-        const bool have = tile < packed_end && (unsigned)page4 < (unsigned)pk.n_pages;
-        const char* p = pk.base + page4 * pk.page_bytes + plane4;  // (no bytes: no address is used)
-        const int c = x * (kMemoryTile * D / 2), s = x * D;
-        codes = rows_rsrc(p + c, have ? pk.plane_bytes() - c : 0);
-        scales = rows_rsrc(p + s, have ? pk.plane_bytes() - s : 0);
-        return have;
+      int page4[PT];
+      auto fetch_page4 = [&](int tile) {
+#pragma unroll
+        for (int u = 0; u < PT; ++u) page4[u] = pages[page_div.div(span.tile(min(tile + kWaves * u, packed_end - 1)) * kMemoryTile)];
       };
-      auto load_k4 = [&](Tile& T) {
+      __amdgpu_buffer_rsrc_t codes[PT], scales[PT];
+      Tile T[PT];
+      auto place4 = [&](int tile) {
+#pragma unroll
+        for (int u = 0; u < PT; ++u) {
+          const int at = tile + kWaves * u, key = span.tile(at) * kMemoryTile;
+          const int x = (key - page_div.div(key) * page_div.d) >> kFewTileBits, c = x * (kMemoryTile * D / 2), s = x * D;
+          T[u].have = at < packed_end && (unsigned)page4[u] < (unsigned)pk.n_pages;
+          const char* p = pk.base + page4[u] * pk.page_bytes + plane4;  // (no bytes: no address is used)
+          codes[u] = rows_rsrc(p + c, T[u].have ? pk.plane_bytes() - c : 0);
+          scales[u] = rows_rsrc(p + s, T[u].have ? pk.plane_bytes() - s : 0);
+        }
+      };
+      auto load_k4 = [&](Tile& T, __amdgpu_buffer_rsrc_t codes, __amdgpu_buffer_rsrc_t scales) {
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
           const int at = k_off + y * (D / 2);
@@ -369,7 +379,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const Args) {
 #pragma unroll
         for (int w = 0; w < KSW; ++w) T.ks[w] = __builtin_amdgcn_raw_buffer_load_b16(scales, ks_off + kBlock * w, 0, ONCE ? kNonTemporal : 0);
       };
-      auto load_v4 = [&](Tile& T) {
+      auto load_v4 = [&](Tile& T, __amdgpu_buffer_rsrc_t codes, __amdgpu_buffer_rsrc_t scales) {
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
           const int at = v_off + n * 64 * VW, as = vs_off + n * 16 * VW;
@@ -406,10 +416,10 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const Args) {
       };
       // A tile's scores of query vector x become probabilities: the running maximum,
       // the accumulators rescaled when it grew, the sum.
-      auto weigh = [&](int x, float (&p)[8]) {
+      auto weigh = [&](int x, float (&p)[NP]) {
         float mx = p[0];
 #pragma unroll
-        for (int j = 1; j < 8; ++j) mx = fmaxf(mx, p[j]);
+        for (int j = 1; j < NP; ++j) mx = fmaxf(mx, p[j]);
         mx = group_max(mx) * sc;
         const bool grow = mx > m[x] + kRescaleLog2;
         if (__ballot(grow)) {
@@ -422,122 +432,131 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const Args) {
         }
         const float ref = m[x] == -INFINITY ? 0.f : m[x];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < NP; ++j) {
           p[j] = __builtin_amdgcn_exp2f(fmaf(p[j], sc, -ref));
           l[x] += p[j];
         }
       };
-      Tile T;
       int tile = first_tile + wave;
       if (tile < packed_end) {
         fetch_page4(tile);
-        T.have = place4(tile);
-        load_k4(T);
-        load_v4(T);
-        fetch_page4(tile + kWaves);
+        place4(tile);
+#pragma unroll
+        for (int u = 0; u < PT; ++u) load_k4(T[u], codes[u], scales[u]);
+#pragma unroll
+        for (int u = 0; u < PT; ++u) load_v4(T[u], codes[u], scales[u]);
+        fetch_page4(tile + PT * kWaves);
       }
 #pragma unroll 1
-      for (; tile < packed_end; tile += kWaves) {
-        const int key0 = span.tile(tile) * kMemoryTile;
-        f32x4 s[NR][2];
+      for (; tile < packed_end; tile += PT * kWaves) {
+        auto key_at = [&](int u) { return span.tile(tile + kWaves * u) * kMemoryTile; };
+        bool have[PT], masked = false;
+        f32x4 s[NR][PT][2];
 #pragma unroll
-        for (int x = 0; x < NR; ++x) s[x][0] = s[x][1] = f32x4{};
+        for (int u = 0; u < PT; ++u) {
+          have[u] = T[u].have;
+          masked = masked || !have[u] || (key_at(u) + kMemoryTile > span.low && key_at(u) < span.high);
 #pragma unroll
-        for (int y = 0; y < 2; ++y)
+          for (int x = 0; x < NR; ++x) s[x][u][0] = s[x][u][1] = f32x4{};
 #pragma unroll
-          for (int w = 0; w < KW; ++w) {
-            const uint32_t ks = T.ks[KW == 8 ? w / 4 : KW == 3 ? w : 0];
-            const bf16x8 kw = decode8(T.k[y][w], y ? scale_of<1>(ks) : scale_of<0>(ks));
+          for (int y = 0; y < 2; ++y)
 #pragma unroll
-            for (int x = 0; x < NR; ++x)
+            for (int w = 0; w < KW; ++w) {
+              const uint32_t ks = T[u].ks[KW == 8 ? w / 4 : KW == 3 ? w : 0];
+              const bf16x8 kw = decode8(T[u].k[y][w], y ? scale_of<1>(ks) : scale_of<0>(ks));
 #pragma unroll
-              for (int z = NT - 1; z >= 0; --z) s[x][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kw, qt[x][w][z], s[x][y], 0, 0, 0);
-          }
-        const bool have = T.have;
-        T.have = place4(tile + kWaves);
-        load_k4(T);
-        fetch_page4(tile + 2 * kWaves);
-        float p[NR][8];
+              for (int x = 0; x < NR; ++x)
+#pragma unroll
+                for (int z = NT - 1; z >= 0; --z)
+                  s[x][u][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kw, qt[x][w][z], s[x][u][y], 0, 0, 0);
+            }
+        }
+        place4(tile + PT * kWaves);
+#pragma unroll
+        for (int u = 0; u < PT; ++u) load_k4(T[u], codes[u], scales[u]);
+        fetch_page4(tile + 2 * PT * kWaves);
+        float p[NR][NP];
 #pragma unroll
         for (int x = 0; x < NR; ++x)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            p[x][2 * i] = s[x][0][i];
-            p[x][2 * i + 1] = s[x][1][i];
-          }
-        const bool masked = !have || (key0 + kMemoryTile > span.low && key0 < span.high);
-        uint32_t vis[NR];  // bit j: key 8 lg + j
+          for (int j = 0; j < NP; ++j) p[x][j] = s[x][j >> 3][j & 1][j >> 1 & 3];
+        uint32_t vis[NR][PT];  // bit j: key 8 lg + j
         if (masked) {
           const Args A = args();
 #pragma unroll
-          for (int x = 0; x < NR; ++x) {
-            vis[x] = have ? ~(uint32_t)hidden_keys(A, q, row[x]).bits(key0, kMemoryTile) : 0u;
-            seen[x] = seen[x] || vis[x];
-            vis[x] >>= 8 * lg;
+          for (int x = 0; x < NR; ++x)
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-              if (!(vis[x] >> j & 1)) p[x][j] = -INFINITY;
-          }
+            for (int u = 0; u < PT; ++u) {
+              vis[x][u] = have[u] ? ~(uint32_t)hidden_keys(A, q, row[x]).bits(key_at(u), kMemoryTile) : 0u;
+              seen[x] = seen[x] || vis[x][u];
+              vis[x][u] >>= 8 * lg;
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                if (!(vis[x][u] >> j & 1)) p[x][8 * u + j] = -INFINITY;
+            }
         } else {
 #pragma unroll
           for (int x = 0; x < NR; ++x) seen[x] = true;
         }
 #pragma unroll
         for (int x = 0; x < NR; ++x) weigh(x, p[x]);
-        // A block of values that is NaN must not reach rows that see none of its keys.
-        if (masked) {
-          uint32_t nan = 0;
 #pragma unroll
-          for (int n = 0; n < NB; ++n)
-#pragma unroll
-            for (int w = 0; w < (VW + 3) / 4; ++w) nan |= ((T.vs[n][w] & 0x7f7f7f7fu) + 0x01010101u) & T.vs[n][w] & 0x80808080u;
-          if (__ballot(nan != 0)) {
+        for (int u = 0; u < PT; ++u) {
+          // A block of values that is NaN must not reach rows that see none of its keys.
+          if (masked) {
+            uint32_t nan = 0;
 #pragma unroll
             for (int n = 0; n < NB; ++n)
 #pragma unroll
-              for (int e = 0; e < VW; ++e) {
-                const uint32_t byte = T.vs[n][e / 4] >> (8 * (e & 3)) & 255;
-                const __bf16 odd = byte == kNanScale ? (__bf16)1.f : (__bf16)0.f;
-                bf16x8 va, pb;
+              for (int w = 0; w < (VW + 3) / 4; ++w) nan |= ((T[u].vs[n][w] & 0x7f7f7f7fu) + 0x01010101u) & T[u].vs[n][w] & 0x80808080u;
+            if (__ballot(nan != 0)) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) va[j] = odd;
-                if (byte == kNanScale) T.vs[n][e / 4] &= ~(255u << (8 * (e & 3)));
+              for (int n = 0; n < NB; ++n)
 #pragma unroll
-                for (int x = 0; x < NR; ++x) {
+                for (int e = 0; e < VW; ++e) {
+                  const uint32_t byte = T[u].vs[n][e / 4] >> (8 * (e & 3)) & 255;
+                  const __bf16 odd = byte == kNanScale ? (__bf16)1.f : (__bf16)0.f;
+                  bf16x8 va, pb;
 #pragma unroll
-                  for (int j = 0; j < 8; ++j) pb[j] = vis[x] >> j & 1 ? (__bf16)1.f : (__bf16)0.f;
-                  const f32x4 c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb, f32x4{}, 0, 0, 0);
+                  for (int j = 0; j < 8; ++j) va[j] = odd;
+                  if (byte == kNanScale) T[u].vs[n][e / 4] &= ~(255u << (8 * (e & 3)));
 #pragma unroll
-                  for (int i = 0; i < 4; ++i)
-                    if (c[i] > 0.f) o[x][n * VW + e][i] = __builtin_nanf("");
+                  for (int x = 0; x < NR; ++x) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) pb[j] = vis[x][u] >> j & 1 ? (__bf16)1.f : (__bf16)0.f;
+                    const f32x4 c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb, f32x4{}, 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                      if (c[i] > 0.f) o[x][n * VW + e][i] = __builtin_nanf("");
+                  }
                 }
-              }
-          }
-        }
-        bf16x8 pb[NR][NT];
-#pragma unroll
-        for (int x = 0; x < NR; ++x)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            float rest = p[x][j];
-#pragma unroll
-            for (int z = 0; z < NT; ++z) {
-              pb[x][z][j] = (__bf16)rest;
-              if (z + 1 < NT) rest -= (float)pb[x][z][j];
             }
           }
+          bf16x8 pb[NR][NT];
 #pragma unroll
-        for (int n = 0; n < NB; ++n)
+          for (int x = 0; x < NR; ++x)
 #pragma unroll
-          for (int e = 0; e < VW; ++e) {
-            const bf16x8 va = decode8(T.v[n][e], v_scale(T, n, e));
+            for (int j = 0; j < 8; ++j) {
+              float rest = p[x][8 * u + j];
 #pragma unroll
-            for (int x = 0; x < NR; ++x)
+              for (int z = 0; z < NT; ++z) {
+                pb[x][z][j] = (__bf16)rest;
+                if (z + 1 < NT) rest -= (float)pb[x][z][j];
+              }
+            }
 #pragma unroll
-              for (int z = NT - 1; z >= 0; --z)
-                o[x][n * VW + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[x][z], o[x][n * VW + e], 0, 0, 0);
-          }
-        load_v4(T);
+          for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int e = 0; e < VW; ++e) {
+              const bf16x8 va = decode8(T[u].v[n][e], v_scale(T[u], n, e));
+#pragma unroll
+              for (int x = 0; x < NR; ++x)
+#pragma unroll
+                for (int z = NT - 1; z >= 0; --z)
+                  o[x][n * VW + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[x][z], o[x][n * VW + e], 0, 0, 0);
+            }
+          load_v4(T[u], codes[u], scales[u]);
+        }
       }
     }
     int tile = t_begin + wave;

@@ -76,13 +76,15 @@ def tol(out, lse, spread, dtype):
 
 def row_hints(case):
     """Values of max_rows that make the call take its other kernels: with the most rows the largest row tiles (or, in
-    bf16 with heads of 128, the kernel for many rows), with some the row tiles of 32."""
+    bf16 with heads of 128, the kernel for many rows), with fewer others."""
     keys = case.max_blocks * case.page
     if case.window:
         keys = min(keys, case.sinks + case.window + 32)
     tiles = max(1.0, len(case.cached) * keys * case.hkv / 32)
-    some = int(200e3 / tiles * 16 / (case.hq // case.hkv)) + 1
-    return (0, 2_000_000) if case.d > 64 else (0, some, 2_000_000)
+    def rows(work):
+        return int(work / tiles * 16 / (case.hq // case.hkv)) + 1
+    # row tiles of 16 and two tiles a step, row tiles of 32, of 64
+    return sorted({0, rows(50e3), rows(200e3), 2_000_000})
 
 
 def check(case, b, layer=1, what="", **kw):

@@ -40,6 +40,19 @@ def test_one_token(b, geo, page):
     check(PackedCase(1, packed, cached, [1] * 6, page, *geo), b)
 
 
+@pytest.mark.parametrize("geo", FAST)
+def test_one_token_in_tables_with_room(b, geo):
+    """Tables that would hold much more: two packed tiles a step, of which the second may be none."""
+    packed = [0, 1, 3, 17, 2, 40]
+    c = PackedCase(20, packed, [9, 32, 100, 17 * 32 + 31, 95, 40 * 32], [1] * 6, 32, *geo)
+    blocks = int(50e3 / 6 / geo[1]) + 1
+    c.table = np.pad(c.table, ((0, 0), (0, blocks)), constant_values=-1)
+    c.max_blocks += blocks
+    check(c, b)
+    c.sinks, c.window = 40, 2 ** 30
+    check(c, b)
+
+
 @pytest.mark.parametrize("geo", FAST + ANY)
 @pytest.mark.parametrize("masked", [False, True])
 def test_several_rows(b, geo, masked):
