@@ -263,3 +263,36 @@ def test_replays_and_two_streams(b):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("geo", [FAST[0], ANY[0]])
+def test_pages_behind_four_gib(b, geo):
+    """Packed pages far into a large pool, in the last of many layers."""
+    from tests.packed_util import tol
+    hq, hkv, d, dtype = geo
+    layers = 36 if d == 128 else 24
+    c = PackedCase(21, [5, 1], [5 * 32 + 9, 40], [2, 1], 32, *geo, layers=layers, sinks=33, window=70)
+    g, pool, batch, q, out, lse = c.dev(b)
+    n = 2 ** 32 // b.packed_page_bytes(g) + c.n4 + 1
+    pages = torch.zeros((n, b.packed_page_bytes(g)), dtype=torch.uint8, device="cuda")
+    pages[n - c.n4:] = torch.from_numpy(c.bits).cuda()
+    table = batch.tensors[2]
+    for r, k in enumerate(c.packed):
+        table[r, :k] += n - c.n4
+    ws = torch.empty(b.tree_attend_packed_workspace(g, batch), dtype=torch.uint8, device="cuda")
+    ref, ref_lse, spread = c.attend_ref(layers - 1)
+    blocks = torch.tensor(c.packed, dtype=torch.int32).cuda()
+    for hint in (0, 2_000_000):
+        batch.c.max_rows = hint
+        out.fill_(7.0)
+        b.tree_attend_packed(g, pool, b.PackedPool(g, pages), layers - 1, batch, blocks, q, out, lse, ws, sinks=33, window=70)
+        assert (np.abs(f64(out) - ref) <= tol(ref, ref_lse, spread, dtype)[0]).all()
+
+
+@pytest.mark.parametrize("geo", MAIN)
+def test_runs_repeat_bit_by_bit(b, geo):
+    """The same call again, with another workspace's contents, gives the same bits."""
+    c = PackedCase(22, [60, 9, 0], [60 * 32 + 3, 300, 77], [3, 1, 2], 32, *geo, sinks=5, window=1500)
+    first = c.run(b)
+    again = c.run(b)
+    assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
