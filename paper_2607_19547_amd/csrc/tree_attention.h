@@ -70,9 +70,14 @@ struct MemoryArgs : SplitArgs {
   int unit_tiles;         // and a unit's start and end as that many
 };
 // Keys of a request that lie in packed pages: whole pages of cached tokens.
+// (SCALAR: of a request that the whole wavefront shares)
+template <bool SCALAR = true>
 __device__ __forceinline__ int packed_keys(const MemoryArgs& a, const Request& q, int b) {
   if (!a.blocks) return 0;
-  return min(min(max(a.blocks[b], 0), a.t.page.div(q.cached)), a.t.max_blocks) * a.t.page.d;
+  int n;
+  if constexpr (SCALAR) n = ((scalar_ptr)(uint64_t)a.blocks)[b];
+  else n = a.blocks[b];
+  return min(min(max(n, 0), a.t.page.div(q.cached)), a.t.max_blocks) * a.t.page.d;
 }
 // Whether a key of the table lies in a page of its pool.
 __device__ __forceinline__ bool in_pool(const MemoryArgs& a, int b, int key, int packed) {
@@ -172,14 +177,14 @@ struct Units {
 __device__ __forceinline__ int key_tiles(const SplitArgs& a, uint32_t keys) {
   return max((int)((keys + (1 << a.tile_bits) - 1) >> a.tile_bits), 1);
 }
-template <bool PAIRS, class A>
+template <bool PAIRS, bool SCALAR = true, class A>
 __device__ __forceinline__ Units unit_sizes(const A& a, const Request& q, int b) {
   Units s;
   s.units = s.nrt = (int)(((int64_t)q.n * a.t.G + (1 << a.row_bits) - 1) >> a.row_bits);
   s.ntile = key_tiles(a, q.len);
   bool whole = true;  // row tiles see everything before them (and are to be paired)
   if constexpr (A::kMemory) {
-    int packed = packed_keys(a, q, b) >> a.tile_bits;
+    int packed = packed_keys<SCALAR>(a, q, b) >> a.tile_bits;
     if (a.window) {
       // the sinks, and as many keys as the windows of a row tile's rows (n - 1 more at most) cover
       const int rows = a.t.mask ? q.n : min(q.n, (int)a.group.div((1 << a.row_bits) - 1) + 2);
@@ -296,7 +301,7 @@ __device__ __forceinline__ bool find_run(const A& a, int w, Run* run) {
     return run->begin < run->total;
   }
   const int lane = threadIdx.x & 63, per = (a.t.B + 63) >> 6;
-  auto tiles = [&](int b) { return request_tiles(a, unit_sizes<PAIRS>(a, load_request(a.t, b), b)); };
+  auto tiles = [&](int b) { return request_tiles(a, unit_sizes<PAIRS, false>(a, load_request(a.t, b), b)); };
   const int b0 = min(lane * per, a.t.B), b1 = min(b0 + per, a.t.B);
   int64_t sum = 0;
 #pragma unroll 4

@@ -249,16 +249,17 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const Args a0) 
       asm volatile("" : "+v"(x));
       const char* from = staged + put_at;
       turn(put_at);
-      const int r = 8 * wave + (x >> 3), c = 2 * (x & 7);
       const u32x2 kc = *(const u32x2*)(from + 8 * x), vc = *(const u32x2*)(from + 512 + 8 * x);
       const float ks = scale_of<0>(*(const uint8_t*)(from + 1024 + 4 * (x & 6) + (x >> 3)));
       const uint32_t vs = *(const uint16_t*)(from + 1056 + 2 * x);
-      *(bf16x8*)(Kd + r * kRow + 16 * (c ^ (r & 15))) = decode8(kc[0], ks);
-      *(bf16x8*)(Kd + r * kRow + 16 * ((c + 1) ^ (r & 15))) = decode8(kc[1], ks);
+      // chunks 2 (x & 7) and the next of key x / 8, channels 2 x and 2 x + 1 of every key
+      const int at_k = ((x >> 3) * kRow) + ((32 * (x & 7)) ^ (16 * (x >> 3)) ^ (128 * (wave & 1))), at_v = 4 * x;
+      char *k_rows = Kd + 8 * wave * kRow, *v_rows = Vd + 8 * wave * kRow;
+      *(bf16x8*)(k_rows + at_k) = decode8(kc[0], ks);
+      *(bf16x8*)(k_rows + (at_k ^ 16)) = decode8(kc[1], ks);
       const bf16x8 v0 = decode8(vc[0], scale_of<0>(vs)), v1 = decode8(vc[1], scale_of<1>(vs));
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        *(bf16x2*)(Vd + (8 * wave + j) * kRow + 16 * ((x >> 2) ^ ((j & 3) << 2)) + 4 * (x & 3)) = bf16x2{v0[j], v1[j]};
+      for (int j = 0; j < 8; ++j) *(bf16x2*)(v_rows + (at_v ^ (64 * (j & 3))) + j * kRow) = bf16x2{v0[j], v1[j]};
     };
     auto fetch = [&](int i, char* Kd, char* Vd) {
       const int key = key_of(i);
