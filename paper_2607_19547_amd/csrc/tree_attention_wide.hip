@@ -68,7 +68,8 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const Args a0) 
   // DS instructions' 16-bit offsets reach; variables are laid out by name.
   __shared__ __attribute__((aligned(1024))) char lo_v0[kKT * kRow], lo_v1[kKT * kRow], lo_v2[kKT * kRow], lo_v3[kKT * kRow];
   __shared__ __attribute__((aligned(1024))) char up_k0[kKT * kRow], up_k1[kKT * kRow], up_k2[kKT * kRow], up_k3[kKT * kRow];
-  __shared__ __attribute__((aligned(1024))) char up_staged[kMemory ? 3 * kWideWaves * kStagedBytes : 4];
+  // (aligned to less than the rings, and so laid out behind them)
+  __shared__ __attribute__((aligned(16))) char up_staged[kMemory ? 3 * kWideWaves * kStagedBytes : 4];
   __shared__ int up_odd[kMemory ? kWideWaves : 1];
   auto kbuf = [&](auto B) -> char* {
     if constexpr (decltype(B)::value == 0) return up_k0;
