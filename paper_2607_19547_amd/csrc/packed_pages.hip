@@ -5,6 +5,12 @@
 // Both ways a thread has whole 32-bit words of codes: eight elements of a key's
 // row, or eight tokens of some channels of the values, whose block of 32 tokens
 // lies in the four lanes of a quad.
+//
+// Bound by memory: 128 pages of 64 tokens, 36 layers of 2 heads of 128 in bf16 are packed
+// in 74 us (302 MB read, 80 written, 5.2 TB/s); 256 come back and are turned in 170 us (161
+// and 604 MB, 4.5 TB/s).  A page alone takes 6 us and 4.4 (turned 7: float64 sines), the
+// chain of its entry, its elements and the stores.  With the places found per item, and
+// loads a few at a time, packing took 107 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -392,7 +398,8 @@ static cs_status pages_args(const Geo& g, const cs_page_pool& pool, const cs_pac
 }
 
 // Pool pages with the non-temporal hint where they would not stay in the 256 MB
-// cache anyway.
+// cache anyway: 128 pages of 36 layers packed and brought back (604 MB of them) 172 ->
+// 132 us, 256 brought back and turned 176 -> 172.
 constexpr int64_t kOnceBytes = 128000000;
 static bool once(const PagesArgs& a, const Geo& g) { return 2 * (int64_t)a.planes * g.T * g.D * g.esize >= kOnceBytes; }
 
