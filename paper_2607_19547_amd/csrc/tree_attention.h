@@ -99,8 +99,9 @@ template <int BITS>
 __device__ __forceinline__ Span span_of(const MemoryArgs& a, const Request& q, int i0, int i1) {
   Span s = {0, 0, 0x7fffffff, 0};
   if (!a.window) return s;
-  const int64_t first = (int64_t)q.cached + 1 + (a.t.mask ? 0 : i0) - a.window;  // the first row's window begins here
-  const int64_t last = (int64_t)q.cached + 1 + (a.t.mask ? q.n - 1 : i1) - a.window;
+  // the first row's window begins here, and the last one's (a row of a mask sees 0 to n rows)
+  const int64_t first = (int64_t)q.cached + (a.t.mask ? 0 : i0 + 1) - a.window;
+  const int64_t last = (int64_t)q.cached + (a.t.mask ? q.n : i1 + 1) - a.window;
   s.sinks = (int)(((int64_t)min(a.sinks, q.len) + (1 << BITS) - 1) >> BITS);
   s.skip = max((int)(min(max(first, (int64_t)0), (int64_t)q.len) >> BITS) - s.sinks, 0);
   s.low = min(a.sinks, q.cached);
@@ -186,7 +187,7 @@ __device__ __forceinline__ Units unit_sizes(const A& a, const Request& q, int b)
   if constexpr (A::kMemory) {
     int packed = packed_keys<SCALAR>(a, q, b) >> a.tile_bits;
     if (a.window) {
-      // the sinks, and as many keys as the windows of a row tile's rows (n - 1 more at most) cover
+      // the sinks, and as many keys as the windows of a row tile's rows cover (as many more as it has rows)
       const int rows = a.t.mask ? q.n : min(q.n, (int)a.group.div((1 << a.row_bits) - 1) + 2);
       const int64_t keys = (int64_t)a.window + rows, tiles = (int64_t)min(a.sinks, q.len) + (1 << a.tile_bits) - 1 >> a.tile_bits;
       s.ntile = (int)min((int64_t)s.ntile, tiles + (keys + (2 << a.tile_bits) >> a.tile_bits));

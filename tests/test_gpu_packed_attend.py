@@ -107,6 +107,15 @@ def test_arbitrary_masks(b, geo):
         check(c, b)
 
 
+@pytest.mark.parametrize("geo", MAIN)
+def test_windows_of_rows_without_rows(b, geo):
+    """A row whose mask is empty sees `window` cached tokens, one more than a row that sees itself: the first of them may
+    be the last of a tile that the other rows' windows leave out."""
+    for packed, cached, window, sinks in (([2, 3], [95, 127], 32, 0), ([0, 5], [31 + 640, 63 + 640], 64, 5)):
+        c = PackedCase(23, packed, cached, [2, 3], 32, *geo, sinks=sinks, window=window, masks=[0, 0b10, 0b111, 0, 0b100])
+        check(c, b)
+
+
 def test_clip_behind_ordinary_pages(b):
     """Many rows with a window and no packed page; pages of 16 and 48 tokens."""
     for geo in (FAST[0], FAST[2], FAST[7]):
