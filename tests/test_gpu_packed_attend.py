@@ -305,3 +305,58 @@ def test_runs_repeat_bit_by_bit(b, geo):
     first = c.run(b)
     again = c.run(b)
     assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+@pytest.mark.parametrize("sinks,window", [(0, 0), (7, 40)])
+def test_full_batch(b, sinks, window):
+    """4,096 requests, most of them over the same packed pages."""
+    from tests.packed_util import tol
+    rng = np.random.default_rng(24)
+    n = 4096
+    packed = [int(x) for x in rng.integers(0, 4, n)]
+    cached = [32 * p + int(x) for p, x in zip(packed, rng.integers(0, 20, n))]
+    c = PackedCase(25, [0] * n, [1] * n, [1] * n, 32, 2, 1, 32, sinks=sinks, window=window, layers=1)
+    c.packed, c.cached = packed, cached
+    from tests.packed_util import random_packed
+    c.n4 = 5
+    c.bits = random_packed(rng, 5, 1, 1, 32, 32)
+    own = c.table[:, 0].copy()
+    c.max_blocks = 6
+    c.table = np.full((n, 6), -1, np.int32)
+    for r in range(n):
+        c.table[r, :packed[r]] = rng.permutation(5)[:packed[r]]
+        c.table[r, packed[r]] = own[r]
+    check(c, b, 0)
+
+
+def test_refused_tensors(b):
+    """What the binding itself refuses, before the library is called."""
+    c = PackedCase(26, [1, 0], [40, 9], [1, 2], 32, *FAST[0])
+    geo, pool, batch, q, out, lse = c.dev(b)
+    bits = torch.from_numpy(c.bits).cuda()
+    packed, blocks = b.PackedPool(geo, bits), torch.tensor(c.packed, dtype=torch.int32).cuda()
+    ws = torch.empty(b.tree_attend_packed_workspace(geo, batch), dtype=torch.uint8, device="cuda")
+    other = b.Geo(3, 16, 2, 128, (16, 24, 24), "bf16", [0, 32])
+    for bad in (bits[:, 1:], bits[:, ::2], bits.to(torch.int32), bits.cpu()):
+        with pytest.raises(ValueError):
+            b.PackedPool(geo, bad)
+    call = lambda **kw: b.tree_attend_packed(*[{**dict(geo=geo, pool=pool, packed=packed, layer=1, batch=batch, blocks=blocks,
+                                                       q=q, out=out, lse=lse, ws=ws), **kw}[k]
+                                               for k in ("geo", "pool", "packed", "layer", "batch", "blocks", "q", "out",
+                                                         "lse", "ws")])
+    for kw in (dict(packed=None), dict(geo=other), dict(blocks=blocks[:1]), dict(blocks=blocks.long()), dict(q=q[:2]),
+               dict(q=q.float()), dict(out=out[:, :3]), dict(lse=lse[:2]), dict(lse=lse.double()), dict(ws=ws.cpu())):
+        with pytest.raises(ValueError):
+            call(**kw)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32).cuda()
+    for args in ((i32(0), i32(0, 1)), (i32(0).long(), i32(0)), (i32(0), i32(0).cpu())):
+        with pytest.raises(ValueError):
+            b.pack_pages(geo, pool, packed, 0, 1, *args)
+        with pytest.raises(ValueError):
+            b.unpack_rebase_pages(geo, packed, pool, 0, 1, *args)
+    with pytest.raises(ValueError):
+        b.unpack_rebase_pages(geo, packed, pool, 0, 1, i32(0), i32(0), i32(1, 2, 3))
+    with pytest.raises(ValueError):
+        b.pack_pages(other, pool, packed, 0, 1, i32(0), i32(0))
+    call()
+    torch.cuda.synchronize()
