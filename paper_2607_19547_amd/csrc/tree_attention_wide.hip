@@ -710,9 +710,16 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const Args a0) 
 // unit's 64 strips are shared by the workgroups of the borders inside it,
 // blockIdx.y among them.  With few pieces a wavefront takes a strip through all
 // of them; with many, four wavefronts take the pieces of a strip in turn.
+//
+// Pieces are loaded in rounds of kRound, a round past the last piece loading it
+// again.  Windows leave units that only two or three pieces share; those load
+// kFewPieces, which takes 9 us where a round of 8 takes 12 (1,999 rows over 1,028
+// keys each), and 13 where it takes 18 (4,000 rows over 4,096).  Sharing the
+// strips among 8 or 16 workgroups a border takes 11 and 16 us instead of 9.
 constexpr int kStripThreads = 256;
 constexpr int kStripShare = 4;
 constexpr int kRound = 8;
+constexpr int kFewPieces = 3;
 template <class Args = SplitArgs>
 __global__ __launch_bounds__(kStripThreads) void tree_combine_wide(const Args a) {
   __shared__ float s_acc[4][8][64], s_m[4][64], s_l[4][64];
@@ -735,26 +742,33 @@ __global__ __launch_bounds__(kStripThreads) void tree_combine_wide(const Args a)
   for (int strip = many ? lot : lot * 4 + grp; strip < strips; strip += borders * kStripShare * (many ? 1 : 4)) {
     const int wave = strip >> 3, c = strip & 7, r = 32 * wave + ql;
     Merge<8> mg;
-    for (int x0 = many ? grp : 0; x0 < pieces; x0 += kRound * step) {
-      float4 st[kRound];
-      f16x8 v16[kRound];
+    auto merge = [&](auto size) {
+      constexpr int kLoads = decltype(size)::value;
+      for (int x0 = many ? grp : 0; x0 < pieces; x0 += kLoads * step) {
+        float4 st[kLoads];
+        f16x8 v16[kLoads];
 #pragma unroll
-      for (int y = 0; y < kRound; ++y) {
-        const int x = min(x0 + y * step, pieces - 1);
-        const int64_t slot = 2 * (int64_t)(w0 + x) + (x == 0);
-        st[y] = *(const float4*)(a.part_ml + (slot * 256 + r) * 4);
-        v16[y] = *(const f16x8*)((const _Float16*)a.part + slot * kPartHalfs + strip * 512 + lane * 8);
+        for (int y = 0; y < kLoads; ++y) {
+          const int x = min(x0 + y * step, pieces - 1);
+          const int64_t slot = 2 * (int64_t)(w0 + x) + (x == 0);
+          st[y] = *(const float4*)(a.part_ml + (slot * 256 + r) * 4);
+          v16[y] = *(const f16x8*)((const _Float16*)a.part + slot * kPartHalfs + strip * 512 + lane * 8);
+        }
+        float2 ml[kLoads];
+        float v[kLoads][8];
+#pragma unroll
+        for (int y = 0; y < kLoads; ++y) {
+          ml[y] = x0 + y * step < pieces ? make_float2(st[y].x, st[y].y) : make_float2(-INFINITY, 0.f);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[y][e] = __builtin_ldexpf((float)v16[y][e], (int)st[y].z);
+        }
+        mg.add(ml, v);
       }
-      float2 ml[kRound];
-      float v[kRound][8];
-#pragma unroll
-      for (int y = 0; y < kRound; ++y) {
-        ml[y] = x0 + y * step < pieces ? make_float2(st[y].x, st[y].y) : make_float2(-INFINITY, 0.f);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[y][e] = __builtin_ldexpf((float)v16[y][e], (int)st[y].z);
-      }
-      mg.add(ml, v);
-    }
+    };
+    if (Args::kMemory && pieces <= kFewPieces)
+      merge(std::integral_constant<int, kFewPieces>{});
+    else
+      merge(std::integral_constant<int, kRound>{});
     if (many) {
       __syncthreads();  // the previous strip has been read
       s_m[grp][lane] = mg.m;
