@@ -670,7 +670,8 @@ cs_status unpack_rebase_pages(const cs_geometry* page, const cs_packed_pool* pac
  * is not finite (a packed block that is NaN makes the keys' scores NaN, or an
  * element of the values).  In float32 scores and outputs over packed pages are
  * float32 too: queries and probabilities go into the products as three bf16
- * terms, which hold all their bits.
+ * terms, which hold all the bits of a magnitude from 2^-110 on, and of a smaller one
+ * all but at most 2^-134.
  *
  *   packed         may be NULL where packed_blocks is
  *   packed_blocks  DEVICE int32 [B], or NULL: no page is packed

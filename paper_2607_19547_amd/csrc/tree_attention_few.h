@@ -309,7 +309,9 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const Args) {
     // 16 x 16 x 32 product, converted to bf16 where it lies.  Row r of the two
     // S^T tiles is key 2 r and key 2 r + 1, so that a lane's scores are those of keys
     // 8 lg .. 8 lg + 7, the eight tokens of its words of values.  In float32 queries
-    // and probabilities are three bf16 terms each, which hold all 24 bits.
+    // and probabilities are three bf16 terms each, which hold all 24 bits from 2^-110 on
+    // (bf16 ends at 2^-133).  A query's first term is cut, not rounded: magnitudes
+    // above 3.39e38 would round to infinity.
     if constexpr (kMemory && D % 32 == 0) {
       constexpr int KW = D / 32, NT = kBf16 ? 1 : 3;
       constexpr int KSW = KW == 8 ? 2 : KW == 3 ? 3 : 1;  // halfwords of key scales that a lane needs
@@ -331,7 +333,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const Args) {
               float rest = __uint_as_float(qf[x][2 * w + (e >> 2)].w[e & 3]);
 #pragma unroll
               for (int y = 0; y < NT; ++y) {
-                qt[x][w][y][e] = (__bf16)rest;
+                qt[x][w][y][e] = (__bf16)(y ? rest : __uint_as_float(__float_as_uint(rest) & 0xffff0000u));
                 rest -= (float)qt[x][w][y][e];
               }
             }
