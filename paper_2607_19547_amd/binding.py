@@ -148,6 +148,18 @@ def _check(code):
         raise CsError(code, lib().cs_last_error().decode())
 
 
+def _int32(x, name):
+    """x as an int of 32 bits (of a larger one ctypes would take the low bits without a word)."""
+    x = int(x)
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError(f"{name} must be a whole number of 32 bits, got {x}")
+    return x
+
+
+def _layers(begin, end):
+    return _int32(begin, "layer_begin"), _int32(end, "layer_end")
+
+
 class Geo:
     """Owns a cs_geometry and the host arrays it points to."""
 
@@ -226,7 +238,7 @@ def score_deviation_topk(geo, k_cache, score_layer, k_fresh, rho, scores, sel_id
     """Scores later-chunk tokens and selects the top rho; returns n_sel."""
     k = ctypes.c_int64(0)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().score_deviation_topk(geo.ref, _ptr(k_cache), int(score_layer), _ptr(k_fresh),
+    _check(lib().score_deviation_topk(geo.ref, _ptr(k_cache), _int32(score_layer, "score_layer"), _ptr(k_fresh),
                                       float(rho), _ptr(scores), _ptr(sel_idx), ctypes.byref(k),
                                       _ptr(workspace), ws_bytes, _stream(stream)))
     return k.value
@@ -234,16 +246,16 @@ def score_deviation_topk(geo, k_cache, score_layer, k_fresh, rho, scores, sel_id
 
 def selective_attend_scatter_workspace(geo, n_sel, n_layers_per_call):
     n = ctypes.c_size_t(0)
-    _check(lib().selective_attend_scatter_workspace(geo.ref, int(n_sel), int(n_layers_per_call),
-                                                    ctypes.byref(n)))
+    _check(lib().selective_attend_scatter_workspace(geo.ref, int(n_sel),
+                                                    _int32(n_layers_per_call, "n_layers_per_call"), ctypes.byref(n)))
     return n.value
 
 
 def selective_attend_scatter(geo, k_cache, v_cache, layer_begin, layer_end, sel_idx, n_sel, q_fresh,
                              k_fresh, v_fresh, out, lse=None, workspace=None, stream=None):
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().selective_attend_scatter(geo.ref, _ptr(k_cache), _ptr(v_cache), int(layer_begin),
-                                          int(layer_end), _ptr(sel_idx), int(n_sel), _ptr(q_fresh),
+    _check(lib().selective_attend_scatter(geo.ref, _ptr(k_cache), _ptr(v_cache), *_layers(layer_begin, layer_end),
+                                          _ptr(sel_idx), int(n_sel), _ptr(q_fresh),
                                           _ptr(k_fresh), _ptr(v_fresh), _ptr(out), _ptr(lse),
                                           _ptr(workspace), ws_bytes, _stream(stream)))
 
@@ -251,8 +263,8 @@ def selective_attend_scatter(geo, k_cache, v_cache, layer_begin, layer_end, sel_
 def selective_attend_scatter_noalloc(geo, k_cache, v_cache, layer_begin, layer_end, sel_idx, n_sel, q_fresh,
                                      k_fresh, v_fresh, out, lse=None, stream=None):
     """selective_attend_scatter with the library's own per-GPU scratch array (no workspace)."""
-    _check(lib().selective_attend_scatter_noalloc(geo.ref, _ptr(k_cache), _ptr(v_cache), int(layer_begin),
-                                                  int(layer_end), _ptr(sel_idx), int(n_sel), _ptr(q_fresh),
+    _check(lib().selective_attend_scatter_noalloc(geo.ref, _ptr(k_cache), _ptr(v_cache),
+                                                  *_layers(layer_begin, layer_end), _ptr(sel_idx), int(n_sel), _ptr(q_fresh),
                                                   _ptr(k_fresh), _ptr(v_fresh), _ptr(out), _ptr(lse),
                                                   _stream(stream)))
 
@@ -287,7 +299,8 @@ def cs_trace_collect():
 
 def selective_attend_scatter_rope_workspace(geo, n_sel, n_layers_per_call):
     n = ctypes.c_size_t(0)
-    _check(lib().selective_attend_scatter_rope_workspace(geo.ref, int(n_sel), int(n_layers_per_call),
+    _check(lib().selective_attend_scatter_rope_workspace(geo.ref, int(n_sel),
+                                                         _int32(n_layers_per_call, "n_layers_per_call"),
                                                          ctypes.byref(n)))
     return n.value
 
@@ -296,8 +309,8 @@ def selective_attend_scatter_rope(geo, k_cache, v_cache, layer_begin, layer_end,
                                   v_fresh, coords, out, lse=None, workspace=None, stream=None):
     """selective_attend_scatter on pre-rotary fresh Q/K, rotated at the global coordinates (DEVICE int32 [T, 3])."""
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().selective_attend_scatter_rope(geo.ref, _ptr(k_cache), _ptr(v_cache), int(layer_begin),
-                                               int(layer_end), _ptr(sel_idx), int(n_sel), _ptr(q_pre), _ptr(k_pre),
+    _check(lib().selective_attend_scatter_rope(geo.ref, _ptr(k_cache), _ptr(v_cache), *_layers(layer_begin, layer_end),
+                                               _ptr(sel_idx), int(n_sel), _ptr(q_pre), _ptr(k_pre),
                                                _ptr(v_fresh), _ptr(coords), _ptr(out), _ptr(lse), _ptr(workspace),
                                                ws_bytes, _stream(stream)))
 
@@ -342,7 +355,8 @@ def score_deviation_topk_paged(geo, k_chunks, score_layer, k_fresh, rho, scores,
                                stream=None):
     k = ctypes.c_int64(0)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().score_deviation_topk_paged(geo.ref, _chunks(k_chunks), int(score_layer), _ptr(k_fresh),
+    _check(lib().score_deviation_topk_paged(geo.ref, _chunks(k_chunks), _int32(score_layer, "score_layer"),
+                                            _ptr(k_fresh),
                                             float(rho), _ptr(scores), _ptr(sel_idx), ctypes.byref(k),
                                             _ptr(workspace), ws_bytes, _stream(stream)))
     return k.value
@@ -351,8 +365,8 @@ def score_deviation_topk_paged(geo, k_chunks, score_layer, k_fresh, rho, scores,
 def selective_attend_scatter_paged(geo, k_chunks, v_chunks, layer_begin, layer_end, sel_idx, n_sel, q_fresh,
                                    k_fresh, v_fresh, out, lse=None, workspace=None, stream=None):
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().selective_attend_scatter_paged(geo.ref, _chunks(k_chunks), _chunks(v_chunks), int(layer_begin),
-                                                int(layer_end), _ptr(sel_idx), int(n_sel), _ptr(q_fresh),
+    _check(lib().selective_attend_scatter_paged(geo.ref, _chunks(k_chunks), _chunks(v_chunks),
+                                                *_layers(layer_begin, layer_end), _ptr(sel_idx), int(n_sel), _ptr(q_fresh),
                                                 _ptr(k_fresh), _ptr(v_fresh), _ptr(out), _ptr(lse),
                                                 _ptr(workspace), ws_bytes, _stream(stream)))
 
@@ -361,7 +375,7 @@ def selective_attend_scatter_rope_paged(geo, k_chunks, v_chunks, layer_begin, la
                                         k_pre, v_fresh, coords, out, lse=None, workspace=None, stream=None):
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(lib().selective_attend_scatter_rope_paged(geo.ref, _chunks(k_chunks), _chunks(v_chunks),
-                                                     int(layer_begin), int(layer_end), _ptr(sel_idx), int(n_sel),
+                                                     *_layers(layer_begin, layer_end), _ptr(sel_idx), int(n_sel),
                                                      _ptr(q_pre), _ptr(k_pre), _ptr(v_fresh), _ptr(coords),
                                                      _ptr(out), _ptr(lse), _ptr(workspace), ws_bytes,
                                                      _stream(stream)))
@@ -422,8 +436,9 @@ class Batch:
             raise ValueError("tree_mask must have at least one word a row")
         self.tensors = (cached_len, row_start, block_table, slot, coords, tree_mask)
         c = self.c = _Batch()
-        c.n_requests, c.n_rows, c.max_blocks, c.max_rows = n, rows, block_table.shape[1], int(max_rows)
-        c.mask_words = 0 if tree_mask is None else tree_mask.shape[1]
+        c.n_requests, c.n_rows = _int32(n, "n_requests"), _int32(rows, "n_rows")
+        c.max_blocks, c.max_rows = _int32(block_table.shape[1], "max_blocks"), _int32(max_rows, "max_rows")
+        c.mask_words = 0 if tree_mask is None else _int32(tree_mask.shape[1], "mask_words")
         c.cached_len = _array(cached_len, "cached_len", "int32", (n,), None)
         dev = self.device = cached_len.get_device()
         c.row_start = _array(row_start, "row_start", "int32", (n + 1,), dev)
@@ -448,7 +463,7 @@ class PagePlan:
         c.n_blocks = _array(n_blocks, "n_blocks", "int32", (n,), dev)
         c.n_blocks_out = _array(n_blocks_out, "n_blocks_out", "int32", (n,), dev)
         c.free_pages = _array(free_pages, "free_pages", "int32", (None,), dev)
-        c.n_free = free_pages.shape[0]
+        c.n_free = _int32(free_pages.shape[0], "n_free")
         c.free_head = _array(free_head, "free_head", "int32", (1,), dev)
         c.free_head_out = _array(free_head_out, "free_head_out", "int32", (1,), dev)
         c.status = _array(status, "status", "int32", (1,), dev)
@@ -496,7 +511,7 @@ def qk_norm_rope_append(geo, pool, layer, batch, q, k, v, q_out, q_weight=None, 
     hq, hkv = geo.g.n_q_heads, geo.g.n_kv_heads
     w = [_array(x, "a weight", geo.g.dtype, (geo.g.head_dim,), batch.device, optional=True)
          for x in (q_weight, k_weight)]
-    _check(lib().qk_norm_rope_append(geo.ref, ctypes.byref(pool.c), int(layer), ctypes.byref(batch.c),
+    _check(lib().qk_norm_rope_append(geo.ref, ctypes.byref(pool.c), _int32(layer, "layer"), ctypes.byref(batch.c),
                                      ctypes.byref(_row_arg(q, "q", geo, batch, hq)),
                                      ctypes.byref(_row_arg(k, "k", geo, batch, hkv)),
                                      ctypes.byref(_row_arg(v, "v", geo, batch, hkv)), w[0], w[1], float(eps),
@@ -518,7 +533,7 @@ def tree_attend_paged(geo, pool, layer, batch, q, out, lse=None, workspace=None,
         raise ValueError("workspace must be contiguous memory of the batch's device")
     if lse is not None and lse.shape[0] < batch.c.n_rows:
         raise ValueError("lse has fewer rows than the batch")
-    _check(lib().tree_attend_paged(geo.ref, ctypes.byref(pool.c), int(layer), ctypes.byref(batch.c),
+    _check(lib().tree_attend_paged(geo.ref, ctypes.byref(pool.c), _int32(layer, "layer"), ctypes.byref(batch.c),
                                    ctypes.byref(_row_arg(q, "q", geo, batch, hq)),
                                    ctypes.byref(_row_arg(out, "out", geo, batch, hq)),
                                    _array(lse, "lse", "float32", (None, hq), batch.device, optional=True),
@@ -529,9 +544,10 @@ def tree_commit_paged(geo, pool, layer_begin, layer_end, batch, accepted, n_acce
                       stream=None):
     """Moves the rows of accepted int32 [B, max_accept] (n_accepted [B] of them) behind the cached tokens."""
     n = batch.c.n_requests
-    _check(lib().tree_commit_paged(geo.ref, ctypes.byref(pool.c), int(layer_begin), int(layer_end),
+    _check(lib().tree_commit_paged(geo.ref, ctypes.byref(pool.c), *_layers(layer_begin, layer_end),
                                    ctypes.byref(batch.c), _array(accepted, "accepted", "int32", (n, None), batch.device),
-                                   accepted.shape[1], _array(n_accepted, "n_accepted", "int32", (n,), batch.device),
+                                   _int32(accepted.shape[1], "max_accept"),
+                                   _array(n_accepted, "n_accepted", "int32", (n,), batch.device),
                                    _array(cached_len_out, "cached_len_out", "int32", (n,), batch.device, optional=True),
                                    _batch_stream(stream, batch, pool, geo)))
 
@@ -564,17 +580,17 @@ def _pages_stream(stream, geo, pool, packed):
 
 def pack_pages(geo, pool, packed, layer_begin, layer_end, src, dst, stream=None):
     """Pages src of the pool into pages dst of the packed pool (int32 tensors [n]), in layers of a range."""
-    n = src.shape[0]
-    _check(lib().pack_pages(geo.ref, ctypes.byref(pool.c), ctypes.byref(packed.c), int(layer_begin), int(layer_end),
+    n = _int32(src.shape[0], "n")
+    _check(lib().pack_pages(geo.ref, ctypes.byref(pool.c), ctypes.byref(packed.c), *_layers(layer_begin, layer_end),
                             _array(src, "src", "int32", (n,), pool.device), _array(dst, "dst", "int32", (n,), pool.device),
                             n, _pages_stream(stream, geo, pool, packed)))
 
 
 def unpack_rebase_pages(geo, packed, pool, layer_begin, layer_end, src, dst, offsets=None, stream=None):
     """Pages src of the packed pool into pages dst of the pool, keys turned by offsets (int32 tensor [n, 3])."""
-    n = src.shape[0]
-    _check(lib().unpack_rebase_pages(geo.ref, ctypes.byref(packed.c), ctypes.byref(pool.c), int(layer_begin),
-                                     int(layer_end), _array(src, "src", "int32", (n,), pool.device),
+    n = _int32(src.shape[0], "n")
+    _check(lib().unpack_rebase_pages(geo.ref, ctypes.byref(packed.c), ctypes.byref(pool.c),
+                                     *_layers(layer_begin, layer_end), _array(src, "src", "int32", (n,), pool.device),
                                      _array(dst, "dst", "int32", (n,), pool.device),
                                      _array(offsets, "offsets", "int32", (n, 3), pool.device, optional=True), n,
                                      _pages_stream(stream, geo, pool, packed)))
@@ -590,6 +606,7 @@ def tree_attend_packed(geo, pool, packed, layer, batch, packed_blocks, q, out, l
                        window=0, stream=None):
     """tree_attend_paged where the first packed_blocks (int32 [B], or None) pages of each request are pages of packed,
     and where, with window > 0, a row sees the first `sinks` and the last `window` of its tokens."""
+    layer, sinks, window = _int32(layer, "layer"), _int32(sinks, "sinks"), _int32(window, "window")
     hq = geo.g.n_q_heads
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     if workspace is not None and (workspace.get_device() != batch.device or not workspace.is_contiguous()):
@@ -601,9 +618,9 @@ def tree_attend_packed(geo, pool, packed, layer, batch, packed_blocks, q, out, l
     if packed is not None:
         _batch_stream(0, batch, packed, geo)
     _check(lib().tree_attend_packed(geo.ref, ctypes.byref(pool.c), None if packed is None else ctypes.byref(packed.c),
-                                    int(layer), ctypes.byref(batch.c),
+                                    layer, ctypes.byref(batch.c),
                                     _array(packed_blocks, "packed_blocks", "int32", (batch.c.n_requests,), batch.device,
-                                           optional=True), int(sinks), int(window),
+                                           optional=True), sinks, window,
                                     ctypes.byref(_row_arg(q, "q", geo, batch, hq)),
                                     ctypes.byref(_row_arg(out, "out", geo, batch, hq)),
                                     _array(lse, "lse", "float32", (None, hq), batch.device, optional=True),
