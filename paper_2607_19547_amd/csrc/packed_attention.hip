@@ -242,7 +242,7 @@ cs_status launch_packed_attend(const Geo& g, const cs_page_pool& pool, const cs_
   a.unit_tiles = 5;
   const Work w = work_of(g, b, job.sinks, job.window);
   if (wide(g, w) && low_o % 16 == 0) {
-    launch_packed_wide(a, ws, false, s);
+    launch_packed_wide(a, ws, s);
     return check_launch("packed attention launch");
   }
   const int nr = row_groups(g, w);

@@ -424,6 +424,6 @@ size_t tree_wide_workspace();
 // of 65,000 tokens 59 -> 62).
 constexpr double kWideOnceBytes = 64e6;
 void launch_tree_wide(SplitArgs a, void* ws, bool once, hipStream_t s);
-void launch_packed_wide(MemoryArgs a, void* ws, bool once, hipStream_t s);
+void launch_packed_wide(MemoryArgs a, void* ws, hipStream_t s);
 
 }  // namespace cs

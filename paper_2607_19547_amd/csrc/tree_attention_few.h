@@ -134,6 +134,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const Args) {
   constexpr int NS = 4 * SUB;                    // scores of a lane per 16 query vectors
   constexpr int kPad = D + 4;
   constexpr bool kMemory = Args::kMemory;
+  static_assert(!(kMemory && ONCE), "packed tiles are loaded without the hint");
   constexpr int kSub = kMemory ? kMemoryTile / KT : 1;  // tiles here of a key tile of the work
   // Where a lane's 16 bytes k of a row lie.  With packed keys they are the elements
   // of its words of codes, which are next to each other (but for D = 96, see there).
@@ -369,17 +370,17 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const Args) {
           if constexpr (kRowRuns) {
 #pragma unroll
             for (int w = 0; w < KW; w += 4) {
-              const auto x = load_words<(KW < 4 ? 4 * KW : 16), ONCE>(codes, at + 4 * w);
+              const auto x = load_words<(KW < 4 ? 4 * KW : 16), false>(codes, at + 4 * w);
 #pragma unroll
               for (int i = 0; i < (KW < 4 ? KW : 4); ++i) T.k[y][w + i] = x.w[i];
             }
           } else {
 #pragma unroll
-            for (int w = 0; w < KW; ++w) T.k[y][w] = load_words<4, ONCE>(codes, at + 16 * w).w[0];
+            for (int w = 0; w < KW; ++w) T.k[y][w] = load_words<4, false>(codes, at + 16 * w).w[0];
           }
         }
 #pragma unroll
-        for (int w = 0; w < KSW; ++w) T.ks[w] = __builtin_amdgcn_raw_buffer_load_b16(scales, ks_off + kBlock * w, 0, ONCE ? kNonTemporal : 0);
+        for (int w = 0; w < KSW; ++w) T.ks[w] = __builtin_amdgcn_raw_buffer_load_b16(scales, ks_off + kBlock * w, 0, 0);
       };
       auto load_v4 = [&](Tile& T, __amdgpu_buffer_rsrc_t codes, __amdgpu_buffer_rsrc_t scales) {
 #pragma unroll
@@ -389,23 +390,23 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attend(const Args) {
           for (int w = 0; w < VW; w += 4) {
             constexpr int last = VW % 4 ? VW % 4 : 4;
             if (w + 4 <= VW) {
-              const auto x = load_words<16, ONCE>(codes, at + 4 * w);
+              const auto x = load_words<16, false>(codes, at + 4 * w);
 #pragma unroll
               for (int i = 0; i < 4; ++i) T.v[n][w + i < VW ? w + i : 0] = x.w[i];
             } else {
-              const auto x = load_words<4 * last, ONCE>(codes, at + 4 * w);
+              const auto x = load_words<4 * last, false>(codes, at + 4 * w);
 #pragma unroll
               for (int i = 0; i < last; ++i) T.v[n][w + i] = x.w[i];
             }
           }
           if constexpr (VW % 4 == 0) {
-            const auto x = load_words<VW, ONCE>(scales, as);
+            const auto x = load_words<VW, false>(scales, as);
 #pragma unroll
             for (int w = 0; w < VW / 4; ++w) T.vs[n][w] = x.w[w];
           } else {
 #pragma unroll
             for (int w = 0; w < VW / 2; ++w) {
-              const uint32_t x = __builtin_amdgcn_raw_buffer_load_b16(scales, as + 2 * w, 0, ONCE ? kNonTemporal : 0);
+              const uint32_t x = __builtin_amdgcn_raw_buffer_load_b16(scales, as + 2 * w, 0, 0);
               if (w & 1) T.vs[n][w / 2] |= x << 16;
               else T.vs[n][w / 2] = x;
             }

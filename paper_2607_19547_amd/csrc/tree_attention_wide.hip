@@ -68,6 +68,7 @@ __device__ __forceinline__ float pair_sum(float x) {
 template <bool ONCE, class Args = SplitArgs>
 __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const Args a0) {
   constexpr bool kMemory = Args::kMemory;
+  static_assert(!(kMemory && ONCE), "memories are loaded without the hint");
   // LDS rows are 256 bytes, a key each, their 16-byte chunks permuted so that
   // the operand reads are free of bank conflicts (K: chunk c of row r at c ^
   // (r & 15); V: at c ^ 4 (r & 3)).  The V ring takes the low 64 KB, where the
@@ -247,8 +248,8 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const Args a0) 
       const int as = x < 8 ? pv.k_scales() + (in_page & 31) + 16 * x - 12 * (x & 1) : pv.v_scales() - 32 + 4 * x;
       char* to = staged + load_at;
       turn(load_at);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rc, (lds_void*)to, 16, at, 0, 0, ONCE ? kNonTemporal : 0);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(to + 1024), 4, as, 0, 0, ONCE ? kNonTemporal : 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rc, (lds_void*)to, 16, at, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(to + 1024), 4, as, 0, 0, 0);
       find_codes(i + 1);
     };
     auto put_codes = [&](char* Kd, char* Vd) {
@@ -562,7 +563,7 @@ __global__ __launch_bounds__(kWideThreads) void tree_attend_wide(const Args a0) 
     // Tile i is in ring slot C, tile i + 1 in N; tile i + 3 goes to S (read last
     // in step i - 1).  Each wavefront waits for its part of tile i + 2 (all but
     // its four newest loads) before the barrier.
-    // (Packed keys: its writes of tile i + 3, too.)
+    // (Packed keys: its writes of tile i + 2, too.)
     auto landed = [&]() {
       if constexpr (kMemory) asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)" ::: "memory");
       else asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
@@ -805,8 +806,8 @@ __global__ __launch_bounds__(kStripThreads) void tree_combine_wide(const Args a)
 
 size_t tree_wide_workspace() { return 2 * (size_t)kWideRuns * (kPartHalfs * sizeof(_Float16) + 4 * 256 * sizeof(float)) + 512; }
 
-template <class Args>
-static void run_wide(Args a, void* ws, bool once, const char* name, const char* combine_name, hipStream_t s) {
+template <bool ONCE, class Args>
+static void run_wide(Args a, void* ws, const char* name, const char* combine_name, hipStream_t s) {
   a.row_bits = kWideRowBits;
   a.tile_bits = kWideTileBits;
   a.run_bits = kWideRunBits;
@@ -818,18 +819,20 @@ static void run_wide(Args a, void* ws, bool once, const char* name, const char* 
   const int runs = most_runs(a);
   {
     TraceScope tr(name, s);
-    if (once) CS_LAUNCH(tr, (tree_attend_wide<true, Args>), dim3((runs + 7) / 8 * 8), dim3(kWideThreads), 0, s, a);
-    else CS_LAUNCH(tr, (tree_attend_wide<false, Args>), dim3((runs + 7) / 8 * 8), dim3(kWideThreads), 0, s, a);
+    const dim3 grid((runs + 7) / 8 * 8);
+    if constexpr (ONCE) CS_LAUNCH(tr, (tree_attend_wide<true, Args>), grid, dim3(kWideThreads), 0, s, a);
+    else CS_LAUNCH(tr, (tree_attend_wide<false, Args>), grid, dim3(kWideThreads), 0, s, a);
   }
   if (runs == 1) return;
   TraceScope tr(combine_name, s);
   CS_LAUNCH(tr, (tree_combine_wide<Args>), dim3(runs - 1, kStripShare), dim3(kStripThreads), 0, s, a);
 }
 void launch_tree_wide(SplitArgs a, void* ws, bool once, hipStream_t s) {
-  run_wide(a, ws, once, "tree_attend_wide", "tree_combine_wide", s);
+  if (once) run_wide<true>(a, ws, "tree_attend_wide", "tree_combine_wide", s);
+  else run_wide<false>(a, ws, "tree_attend_wide", "tree_combine_wide", s);
 }
-void launch_packed_wide(MemoryArgs a, void* ws, bool once, hipStream_t s) {
-  run_wide(a, ws, once, "packed_attend_wide", "packed_combine_wide", s);
+void launch_packed_wide(MemoryArgs a, void* ws, hipStream_t s) {
+  run_wide<false>(a, ws, "packed_attend_wide", "packed_combine_wide", s);
 }
 
 }  // namespace cs
