@@ -140,18 +140,24 @@ static bool has_instance(const Geo& g) {
 }
 
 // Which kernel and row tile takes a batch, by the key tiles (of 32, over all requests
-// and KV heads) that the block tables have room for and the windows let be seen, and the
-// row tiles of 16 query vectors that each of them meets.  The host does not know the
-// lengths, and tables are seldom filled: borders are put at 1.6 times what was
-// measured on filled ones.
+// and KV heads) that a row tile of each may see, the row tiles of 16 query vectors that
+// each of them meets, and the units (row tiles of all requests and KV heads), whose
+// starts and ends count where they are short.  The host does not know the lengths, and
+// tables are seldom filled: keys are taken to fill 1 / 1.6 of their room.  What a window
+// leaves is known, and taken as it is.
+constexpr double kRoom = 1.6;
 struct Work {
   double tiles, row_tiles, row_tiles_wide;  // (of 256)
+  double units, units_wide;
+  bool window;                              // that bounds the tiles
 };
 static Work work_of(const Geo& g, const cs_batch& b, int sinks, int window) {
   const double rows = b.max_rows > 0 ? b.max_rows : b.n_rows, vectors = rows * g.G;
-  double keys = (double)b.max_blocks * g.T;
-  if (window) keys = std::min(keys, (double)sinks + window + std::min(rows, 32.));  // (a row tile's rows, about)
-  return {b.n_requests * keys * g.Hkv / 32, ceil(vectors / 16), ceil(vectors / 256)};
+  const double row_tiles = ceil(vectors / 16), heads = (double)b.n_requests * g.Hkv;
+  const double keys = (double)b.max_blocks * g.T / kRoom;
+  const double seen = window ? (double)sinks + window + std::min(rows, 32.) : keys;  // (with a row tile's rows, about)
+  return {heads * std::min(keys, seen) / 32, row_tiles, ceil(vectors / 256), heads * row_tiles, heads * ceil(vectors / 256),
+          seen < keys};
 }
 // Row tiles of 32 or 64 convert a packed tile half or a quarter as often, in fewer and
 // longer pieces of work.  Measured, tiles x row tiles of 16 and us with row tiles of 16 /
@@ -160,28 +166,40 @@ static Work work_of(const Geo& g, const cs_batch& b, int sinks, int window) {
 // x 96 9,000 21.8 / 22.4, 19,000 33.0 / 30.3, 131,000 121 / 77; float32 x 64 67,000 51.6 / 51.5,
 // 131,000 78.7 / 76.2; x 32 66,000 43.9 / 41.2 / 47.9, 131,000 66.3 / 60.6 / 63.8.  Row tiles of 32
 // spill registers with bf16 x 128 (which has the kernel for many rows), x 256 and float32 x 128.
+// With windows the start and end of a unit, beyond the two that a request and KV head have in any
+// case, weigh as 25 tiles.  Bf16 x 64, x 96, float32 x 64: 1,000 rows that see 1,024 keys each 44.4 /
+// 38.5, 52.7 / 45.9, 72.3 / 66.4; 250 rows that see 4,096 27.8 / 27.8, 43.7 / 35.9, 33.8 / 35.8; 512 requests of
+// 8 rows that see 128 89 / 87, 106 / 97, 100 / 101, of 3 rows 61 / 67, 70 / 72, 66 / 73.
 static int most_row_groups(const Geo& g) {
   if (g.dtype == CS_F32) return g.D <= 64 ? 2 : 1;
   return g.D <= 64 ? 4 : g.D <= 96 ? 2 : 1;
 }
 static int row_groups(const Geo& g, const Work& w) {
-  const double n = w.tiles * w.row_tiles;
-  if (w.row_tiles <= 1 || n < 1.6 * (g.D == 96 ? 12e3 : 55e3)) return 1;
-  return std::min(most_row_groups(g), n < 1.6 * 200e3 ? 2 : 4);
+  const double n = w.tiles * w.row_tiles, ends = w.window ? 25 * w.units * (1 - 2 / w.row_tiles) : 0;
+  if (w.row_tiles <= 1 || n + ends < (g.D == 96 ? 12e3 : 55e3)) return 1;
+  return std::min(most_row_groups(g), n < 200e3 ? 2 : 4);
 }
 // Two packed tiles a step, with row tiles of 16, in place of one.  Measured (us, tiles of
 // memories that the cache does not hold, one / two): 12,000 23.7 / 26.0, 25,000 35.2 / 33.8,
 // 33,000 48 / 41, 66,000 72 / 67 and 77 / 68; x 64 66,000 50 / 44, float32 x 64 50 / 47; x 32 36.2 / 36.3.
-constexpr double kDeepTiles = 1.6 * 25e3;
+constexpr double kDeepTiles = 25e3;
 constexpr bool has_deep(bool bf16, int d) { return d == 64 || (bf16 && (d == 96 || d == 128)); }
-// The kernel for many rows (bf16 x 128) takes 5 ns for a key tile and 256 query vectors
-// on the whole GPU, row tiles of 16 take 0.56 ns each, and it starts and ends 10 us
-// later.  Measured (us, row tiles of 16 / it): 65,536 tokens, 17 rows 38.6 / 45.4, 64 rows
-// 84 / 62; 16,384 tokens, 64 rows 31.7 / 36.6; 8 requests of 4,096, 64 rows 53 / 46; 32 of
-// 8,192, 4 rows 35 / 69; 8,192 tokens, 250 rows 56 / 46; 1,024 tokens, 250 rows 23.1 / 25.6; 1,999 rows
-// that see 1,024 tokens each 109 / 54 (8 query heads for each of 2).
-static bool wide(const Geo& g, const Work& w) {
-  return g.dtype == CS_BF16 && g.D == 128 && w.tiles * (0.56 * w.row_tiles - 5 * w.row_tiles_wide) > 1.6 * 10e3;
+// The kernel for many rows (bf16 x 128) starts and ends 11 us later than row tiles of 16.  A
+// key tile of 32 takes it 2.7 ns for 256 query vectors, on the whole GPU, and a unit 50 ns; row
+// tiles of 16 take 0.55 ns a tile, of ordinary pages 1.2 (whether there are other than ordinary ones
+// is known, how many is not), and 15 ns a unit: fitted to 238 batches of 1 to 48 requests and 2 to
+// 2,000 rows, of which the rule takes the faster side, or one within 5% of it, in all but 6, the worst
+// 16% off; of 41 others, of 64 to 4,096 requests, in all but 4 (11%).
+// Measured (us, row tiles of 16 / many rows; 16 / 2 heads): 65,536 tokens, 17 rows 36.4 / 42.8, 64 rows 77 /
+// 58; 16,384, 64 rows 32.0 / 32.5; 8,192, 250 rows 49.8 / 40.5; 1,024, 250 rows 22.5 / 25.3; 8 requests of
+// 4,096, 64 rows 45 / 43; 32 of 8,192, 4 rows 35 / 66; 39 of 768, 27 rows 43.6 / 32.0.  Rows that see
+// 1,024 keys each, ordinary and packed: 250 rows 28.9 / 28.7 and 25.2 / 30.5, 500 39.7 / 29.5 and 34.2 / 31.2, 1,950
+// 106 / 47.5 and 110 / 51.8; 256 keys: 250 rows 18.8 / 28.8 and 19.9 / 30.5, 1,000 36.7 / 30.5 and 39.1 / 31.9; 4,096
+// keys: 64 rows 27.9 / 26.3 and 20.6 / 28.1, 1,000 169 / 59 and 106 / 63; 48 requests of 16 rows 246 / 71 and 84 / 65.
+static bool wide(const Geo& g, const Work& w, bool all_paged) {
+  const double few = (all_paged ? 1.2 : 0.55) * w.tiles * w.row_tiles + 15 * w.units;  // ns
+  const double many = 2.7 * w.tiles * w.row_tiles_wide + 50 * w.units_wide;
+  return g.dtype == CS_BF16 && g.D == 128 && few - many > 11e3;
 }
 
 size_t packed_attend_workspace(const Geo& g) {
@@ -241,7 +259,7 @@ cs_status launch_packed_attend(const Geo& g, const cs_page_pool& pool, const cs_
   a.paged_bits = 0;
   a.unit_tiles = 5;
   const Work w = work_of(g, b, job.sinks, job.window);
-  if (wide(g, w) && low_o % 16 == 0) {
+  if (wide(g, w, !job.blocks) && low_o % 16 == 0) {
     launch_packed_wide(a, ws, s);
     return check_launch("packed attention launch");
   }
