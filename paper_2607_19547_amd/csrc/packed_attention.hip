@@ -179,11 +179,14 @@ static int row_groups(const Geo& g, const Work& w) {
   if (w.row_tiles <= 1 || n + ends < (g.D == 96 ? 12e3 : 55e3)) return 1;
   return std::min(most_row_groups(g), n < 200e3 ? 2 : 4);
 }
-// Two packed tiles a step, with row tiles of 16, in place of one.  Measured (us, tiles of
-// memories that the cache does not hold, one / two): 12,000 23.7 / 26.0, 25,000 35.2 / 33.8,
-// 33,000 48 / 41, 66,000 72 / 67 and 77 / 68; x 64 66,000 50 / 44, float32 x 64 50 / 47; x 32 36.2 / 36.3.
-constexpr double kDeepTiles = 25e3;
-constexpr bool has_deep(bool bf16, int d) { return d == 64 || (bf16 && (d == 96 || d == 128)); }
+// Two packed tiles a step, with row tiles of 16, in place of one: more in flight where
+// much is read.  Measured (us, tiles x row tiles of memories that the cache does not hold, one / two):
+// bf16 x 128 16,400 24.8 / 25.2, 33,000 38.8 / 39.3, 66,000 60.6 / 56.8, 131,000 105 / 96; x 64 33,000
+// 25.7 / 24.5, 66,000 46.4 / 40.5, 131,000 80.5 / 67.6; float32 x 64 33,000 28.8 / 28.8, 66,000 49.5 / 45.6;
+// windows of 8,192 keys, 64 rows, 33,000 43.7 / 43.4, 30.6 / 30.2, 33.1 / 34.2; x 32 no change; bf16 x 96
+// 66,000 67.4 / 75.3, 131,000 121 / 134: there always one.
+constexpr double kDeepTiles = 30e3;
+constexpr bool has_deep(bool bf16, int d) { return d == 64 || (bf16 && d == 128); }
 // The kernel for many rows (bf16 x 128) starts and ends 11 us later than row tiles of 16.  A
 // key tile of 32 takes it 2.7 ns for 256 query vectors, on the whole GPU, and a unit 50 ns; row
 // tiles of 16 take 0.55 ns a tile, of ordinary pages 1.2 (whether there are other than ordinary ones
