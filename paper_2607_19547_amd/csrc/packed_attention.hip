@@ -169,7 +169,8 @@ static Work work_of(const Geo& g, const cs_batch& b, int sinks, int window) {
 // With windows the start and end of a unit, beyond the two that a request and KV head have in any
 // case, weigh as 25 tiles.  Bf16 x 64, x 96, float32 x 64: 1,000 rows that see 1,024 keys each 44.4 /
 // 38.5, 52.7 / 45.9, 72.3 / 66.4; 250 rows that see 4,096 27.8 / 27.8, 43.7 / 35.9, 33.8 / 35.8; 512 requests of
-// 8 rows that see 128 89 / 87, 106 / 97, 100 / 101, of 3 rows 61 / 67, 70 / 72, 66 / 73.
+// 8 rows that see 128 89 / 87, 106 / 97, 100 / 101, of 3 rows 61 / 67, 70 / 72, 66 / 73.  32 query vectors
+// fill half of a row tile of 64: 64 requests of 65,536 tokens, 3 rows, x 64 164 / 226, x 32 171 / 225 (32 / 64).
 static int most_row_groups(const Geo& g) {
   if (g.dtype == CS_F32) return g.D <= 64 ? 2 : 1;
   return g.D <= 64 ? 4 : g.D <= 96 ? 2 : 1;
@@ -177,7 +178,7 @@ static int most_row_groups(const Geo& g) {
 static int row_groups(const Geo& g, const Work& w) {
   const double n = w.tiles * w.row_tiles, ends = w.window ? 25 * w.units * (1 - 2 / w.row_tiles) : 0;
   if (w.row_tiles <= 1 || n + ends < (g.D == 96 ? 12e3 : 55e3)) return 1;
-  return std::min(most_row_groups(g), n < 200e3 ? 2 : 4);
+  return std::min(most_row_groups(g), n < 200e3 || w.row_tiles <= 2 ? 2 : 4);
 }
 // Two packed tiles a step, with row tiles of 16, in place of one: more in flight where
 // much is read.  Measured (us, tiles x row tiles of memories that the cache does not hold, one / two):
