@@ -184,8 +184,8 @@ static int row_groups(const Geo& g, const Work& w) {
 // much is read.  Measured (us, tiles x row tiles of memories that the cache does not hold, one / two):
 // bf16 x 128 16,400 24.8 / 25.2, 33,000 38.8 / 39.3, 66,000 60.6 / 56.8, 131,000 105 / 96; x 64 33,000
 // 25.7 / 24.5, 66,000 46.4 / 40.5, 131,000 80.5 / 67.6; float32 x 64 33,000 28.8 / 28.8, 66,000 49.5 / 45.6;
-// windows of 8,192 keys, 64 rows, 33,000 43.7 / 43.4, 30.6 / 30.2, 33.1 / 34.2; x 32 no change; bf16 x 96
-// 66,000 67.4 / 75.3, 131,000 121 / 134: there always one.
+// windows of 8,192 keys, 64 requests, 33,000 (bf16 x 128, x 64, float32 x 64) 43.7 / 43.4, 30.6 / 30.2, 33.1 /
+// 34.2; x 32 no change; bf16 x 96 66,000 67.4 / 75.3, 131,000 121 / 134: there always one.
 constexpr double kDeepTiles = 30e3;
 constexpr bool has_deep(bool bf16, int d) { return d == 64 || (bf16 && d == 128); }
 // The kernel for many rows (bf16 x 128) starts and ends 11 us later than row tiles of 16.  A
