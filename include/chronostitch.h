@@ -598,8 +598,9 @@ cs_status tree_commit_paged(const cs_geometry* page, const cs_page_pool* pool, i
  * of 32 shares.  Blocks lie along a token's row for keys, and along 32 tokens of
  * a channel for values.  With amax the largest magnitude in the block, e is the
  * least from -125 to 125 with amax <= 7 x 2^e (beyond 6 x 2^e saturating costs no more
- * than rounding costs at 5), elements are rounded to nearest, ties to the even
- * code.  A block that holds an infinity or a NaN is NaN altogether, and no other
+ * than rounding costs at 5), or 125 where amax is above 7 x 2^125; elements are rounded
+ * to nearest, ties to the even code, and what is larger than 6 x 2^e saturates there.
+ * A block that holds an infinity or a NaN is NaN altogether, and no other
  * block is.
  *
  * A packed page is [L][H_kv] planes of 17/16 x P x D bytes each:

@@ -9,7 +9,7 @@ VALUES = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
 
 
 def exponent(amax):
-    """The least e from -125 to 125 with amax <= 7 x 2^e."""
+    """The least e from -125 to 125 with amax <= 7 x 2^e, or 125 where there is none."""
     e = -125
     while e < 125 and amax > 7.0 * 2.0 ** e:
         e += 1

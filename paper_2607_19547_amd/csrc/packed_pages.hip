@@ -89,7 +89,8 @@ __device__ __forceinline__ int item_at(const Share& s, const FastDiv& per_plane,
 }
 
 // One block's scale byte from the bits of its largest magnitude (float32; an
-// infinity or NaN has the largest of all): the least e with amax <= 7 x 2^e.
+// infinity or NaN has the largest of all): the least e from -125 to 125 with amax <=
+// 7 x 2^e, or 125 (codes saturate).
 __device__ __forceinline__ uint32_t scale_byte(uint32_t amax) {
   const int e = (int)((amax + 0x1fffffu) >> 23) - 2;  // (1.75 = 7 / 4 has the mantissa 0x600000)
   return amax >= 0x7f800000u ? kNanScale : (uint32_t)min(max(e, kLeastScale), kMostScale);
