@@ -7,8 +7,8 @@
 // first row's window is left out of its count, so runs stay even.
 //
 // Few rows are bound by memory: 64 requests of up to 32,768 packed tokens, one row, 16 / 2
-// heads of 128 (234 MB) 50 us and 5 for the merge, 4.6 TB/s.  One row over 8,192 tokens takes
-// 7.0 us and 3.9 (two launches' chains of loads).  What many rows are bound by is told
+// heads of 128 (234 MB) 51 us and 6 for the merge, 4.6 TB/s.  One row over 8,192 tokens takes
+// 7.1 us and 4.2 (two launches' chains of loads).  What many rows are bound by is told
 // in tree_attention_wide.hip.
 #include <math.h>
 

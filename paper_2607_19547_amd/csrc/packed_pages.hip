@@ -7,8 +7,8 @@
 // lies in the four lanes of a quad.
 //
 // Bound by memory: 128 pages of 64 tokens, 36 layers of 2 heads of 128 in bf16 are packed
-// in 74 us (302 MB read, 80 written, 5.2 TB/s); 256 come back and are turned in 170 us (161
-// and 604 MB, 4.5 TB/s).  A page alone takes 6 us and 4.4 (turned 7: float64 sines), the
+// in 74 us (302 MB read, 80 written, 5.2 TB/s); 256 come back and are turned in 171 us (161
+// and 604 MB, 4.5 TB/s).  A page alone takes 6.4 us and 4.8 (turned 7.4: float64 sines), the
 // chain of its entry, its elements and the stores.  With the places found per item, and
 // loads a few at a time, packing took 107 us.
 #include <algorithm>

@@ -30,8 +30,9 @@
 // Memories in packed pages, and windows (MemoryArgs).  Packed tiles come as codes, a
 // quarter of the bytes, and are converted on their way into the ring: 16 conversions a
 // wavefront and tile, which with the exponentials bind the loop (two questions of 389 rows over
-// 32,768 packed tokens 228 us; without the conversions 195).  Codes go by LDS, for
-// want of registers (in registers across a step: 299 us where this took 253).
+// 32,768 packed tokens 223 us in a row, 264 with pauses between; without the conversions 195 where
+// it took 228).  Codes go by LDS, for want of registers (in registers across a step: 299 us where
+// this took 253).
 #include <math.h>
 
 #include <type_traits>
