@@ -150,13 +150,16 @@ def _check(code):
 
 def _int32(x, name):
     """x as an int of 32 bits (of a larger one ctypes would take the low bits without a word)."""
-    x = int(x)
-    if not -2 ** 31 <= x < 2 ** 31:
-        raise ValueError(f"{name} must be a whole number of 32 bits, got {x}")
-    return x
+    if type(x) is not int:
+        x = int(x)
+    if -0x80000000 <= x <= 0x7fffffff:
+        return x
+    raise ValueError(f"{name} must be a whole number of 32 bits, got {x}")
 
 
 def _layers(begin, end):
+    if type(begin) is type(end) is int and 0 <= begin <= end <= 0x7fffffff:  # (0.1 us less than one by one)
+        return begin, end
     return _int32(begin, "layer_begin"), _int32(end, "layer_end")
 
 
@@ -581,7 +584,8 @@ def _pages_stream(stream, geo, pool, packed):
 def pack_pages(geo, pool, packed, layer_begin, layer_end, src, dst, stream=None):
     """Pages src of the pool into pages dst of the packed pool (int32 tensors [n]), in layers of a range."""
     n = _int32(src.shape[0], "n")
-    _check(lib().pack_pages(geo.ref, ctypes.byref(pool.c), ctypes.byref(packed.c), *_layers(layer_begin, layer_end),
+    begin, end = _layers(layer_begin, layer_end)
+    _check(lib().pack_pages(geo.ref, ctypes.byref(pool.c), ctypes.byref(packed.c), begin, end,
                             _array(src, "src", "int32", (n,), pool.device), _array(dst, "dst", "int32", (n,), pool.device),
                             n, _pages_stream(stream, geo, pool, packed)))
 
@@ -589,8 +593,9 @@ def pack_pages(geo, pool, packed, layer_begin, layer_end, src, dst, stream=None)
 def unpack_rebase_pages(geo, packed, pool, layer_begin, layer_end, src, dst, offsets=None, stream=None):
     """Pages src of the packed pool into pages dst of the pool, keys turned by offsets (int32 tensor [n, 3])."""
     n = _int32(src.shape[0], "n")
+    begin, end = _layers(layer_begin, layer_end)
     _check(lib().unpack_rebase_pages(geo.ref, ctypes.byref(packed.c), ctypes.byref(pool.c),
-                                     *_layers(layer_begin, layer_end), _array(src, "src", "int32", (n,), pool.device),
+                                     begin, end, _array(src, "src", "int32", (n,), pool.device),
                                      _array(dst, "dst", "int32", (n,), pool.device),
                                      _array(offsets, "offsets", "int32", (n, 3), pool.device, optional=True), n,
                                      _pages_stream(stream, geo, pool, packed)))
